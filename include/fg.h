@@ -63,7 +63,8 @@ typedef enum {
   FG_ERR_DEVICE = -5       /* a HIP runtime call failed (see fg_last_device_error) */
 } fg_status;
 
-typedef enum { FG_F16 = 0, FG_Q4G64 = 1, FG_Q4G64_TILED = 2, FG_Q4G64_H16 = 3, FG_Q4G64_H16_TILED = 4 } fg_dtype;
+typedef enum { FG_F16 = 0, FG_Q4G64 = 1, FG_Q4G64_TILED = 2, FG_Q4G64_H16 = 3, FG_Q4G64_H16_TILED = 4,
+               FG_I8P64 = 5 } fg_dtype;
 
 /* A weight matrix [rows = output features, cols = input features], row-major.
  * FG_F16:   data = FP16 values, meta = NULL.
@@ -118,11 +119,14 @@ typedef struct {
  *   k_codes/v_codes [n_pages][nh][64][dh/2] bytes, k_meta/v_meta [n_pages][nh][64][dh/64] pairs
  * (8-byte pairs for FG_Q4G64, 4-byte FP16 pairs for FG_Q4G64_H16).  FG_F16 pages hold plain FP16 rows,
  * k_codes/v_codes [n_pages][nh][64][dh] halves, metas NULL.
- * Rows are stored exactly as in fg_kv_cache; only their place differs. */
+ * FG_I8P64 pages: k_codes [n_pages][nh][64][dh] bytes; v_codes [n_pages][nh][4][dh][16] bytes (16 consecutive
+ * positions of one head dimension lie next to each other: the order in which the matrix cores contract over
+ * positions); k_meta/v_meta [n_pages][nh] binary32 scales (4-byte aligned).
+ * In the other formats rows are stored exactly as in fg_kv_cache; only their place differs. */
 #define FG_PAGE_ROWS 64
 typedef struct {
   void *k_codes, *k_meta, *v_codes, *v_meta; /* device */
-  int32_t dtype;                             /* FG_Q4G64, FG_Q4G64_H16 or FG_F16 */
+  int32_t dtype;                             /* FG_Q4G64, FG_Q4G64_H16, FG_F16 or FG_I8P64 */
   int32_t n_pages;
 } fg_kv_pages;
 
@@ -311,7 +315,11 @@ size_t fg_workspace_bytes(const fg_model_cfg* cfg, const fg_layer_weights* layer
 
 /* ---- Appendix, "Diagonal block schedule": paged cache, sequences at different steps --------
  * fg_kv_append_paged: like fg_kv_append, rows [b, s, h1]; row j of sequence i goes to position
- * pos[i] + j of sequence seq_ids[i], through the page table. */
+ * pos[i] + j of sequence seq_ids[i], through the page table.  FG_I8P64 pages: a sequence that seq_ids names more than
+ * once is appended to in the order of the rows i; two DIFFERENT sequences of one call whose tables name the same page
+ * for the positions written leave that page's contents undefined (fg_beam_reorder_paged gives every beam a page of
+ * its own there).  For attention with fewer cache heads than query heads, pass a cfg of the cache's heads
+ * (h1 = nkv * dh, nh = nkv). */
 int fg_kv_append_paged(const fg_model_cfg* cfg, const void* k_f16, const void* v_f16, int64_t row_stride,
                        int32_t b, int32_t s, const fg_kv_pages* pages, const fg_ragged* seqs, void* stream);
 
@@ -322,6 +330,28 @@ int fg_kv_append_paged(const fg_model_cfg* cfg, const void* k_f16, const void* v
 int fg_decode_attention_paged(const fg_model_cfg* cfg, const void* q_f16, int64_t q_row_stride, int32_t b,
                               const fg_kv_pages* pages, const fg_ragged* seqs, int32_t rows_bias,
                               void* out_f16, void* stream);
+
+/* The same for 8-bit pages (FG_I8P64; FG_ERR_UNSUPPORTED otherwise), with two liberties more.
+ * nkv cache heads for cfg->nh query heads (cfg->nh % nkv == 0; pages are [n_pages][nkv]...): query head h reads cache
+ * head h / (nh / nkv).
+ * beams: rows i*beams .. i*beams + beams-1 (b % beams == 0, beams <= FG_MAX_BEAMS) are expected to share pages, as
+ * the beams of one sequence share those of its prompt: a page that several of them name for the same positions is
+ * read once.  Results do not depend on `beams`, up to the order of sums; any mixture of shared and own pages is right.
+ * ws (FG_ERR_WORKSPACE without it) holds the partial results of long sequences that are split over workgroups; sized
+ * for b rows and tables of table_stride pages.  The other calls on 8-bit pages (fg_decode_attention_paged, the paged
+ * layers, fg_generate_diagonal) run the same kernel with beams = 1, nkv = nh. */
+#define FG_MAX_BEAMS 16
+int fg_decode_attention_beams_paged(const fg_model_cfg* cfg, int32_t nkv, int32_t beams, const void* q_f16,
+                                    int64_t q_row_stride, int32_t b, const fg_kv_pages* pages, const fg_ragged* seqs,
+                                    int32_t rows_bias, void* out_f16, void* ws, size_t ws_bytes, void* stream);
+size_t fg_decode_attention_beams_workspace_bytes(const fg_model_cfg* cfg, int32_t nkv, int32_t beams, int32_t b,
+                                                 int32_t table_stride);
+
+/* Rows of a paged cache as FP16, any page format: row j of k_out, v_out [b, s, h1] (consecutive rows row_stride
+ * elements apart, a multiple of 8) is what position pos[i] + j of sequence seq_ids[i] holds: its value rounded to
+ * binary32 and then to FP16 (seqs->pos NULL: from position 0).  Positions that the table or the pool does not have (see fg_ragged) give zeros. */
+int fg_kv_gather_paged(const fg_model_cfg* cfg, const fg_kv_pages* pages, const fg_ragged* seqs, int32_t b, int32_t s,
+                       void* k_out_f16, void* v_out_f16, int64_t row_stride, void* stream);
 
 /* Top-K sparse attention (Section 5) over a paged cache with a length per sequence: as
  * fg_decode_attention_paged, but row i keeps only its min(topk, rows of row i) highest-weighted rows of
@@ -372,6 +402,46 @@ size_t fg_diagonal_workspace_bytes(const fg_model_cfg* cfg, const fg_layer_weigh
  * arguments).  The block schedule needs n_seqs * ceil((s + n) / 64). */
 int64_t fg_diagonal_pages_needed(int32_t n_seqs, int32_t s, int32_t n, int32_t gpu_batch_size);
 
+/* ---- Beam search ---------------------------------------------------------------------------
+ * n_groups sequences with `beams` rows each (1 <= beams <= FG_MAX_BEAMS); row g*beams + j is beam j of sequence g.
+ *
+ * fg_beam_select: of all continuations (beam j, word w) of a sequence, worth
+ *   v = scores[j] + logits[j][w] - log(sum over w' of exp(logits[j][w'])),
+ * the n_best (1 .. FG_MAX_BEST) of the largest v, in descending order; among equal ones the larger logit, then the
+ * lowest j * vocab + w comes first.  v is compared in binary64 and returned in binary32.
+ * logits: binary32 rows of cfg->vocab words, row_stride >= vocab elements apart (what fg_lm_head_greedy leaves).
+ * A logit of -inf or NaN is no continuation (a forbidden word), +inf counts as the largest binary32 number; scores of
+ * -inf or NaN take the beam out.  done (int32 per row, NULL: none): a beam with done != 0 offers itself once, as word
+ * `eos` (0 <= eos < vocab, else FG_ERR_SHAPE) at its own score, and its logits do not matter.
+ * Outputs, [n_groups][n_best]: the beam 0 .. beams-1 continued, the word, its v, and (NULL: not wanted) out_done =
+ * done of the beam, or word == eos (eos < 0: never).  Where there are fewer continuations than n_best, the rest are
+ * beam -1, word -1, v = -inf, done 1.  ws >= fg_beam_select_workspace_bytes. */
+#define FG_MAX_BEST 32
+int fg_beam_select(const fg_model_cfg* cfg, int32_t n_groups, int32_t beams, int32_t n_best, const float* logits,
+                   int64_t row_stride, const float* scores, const int32_t* done, int32_t eos, int32_t* out_beams,
+                   int32_t* out_ids, float* out_scores, int32_t* out_done, void* ws, size_t ws_bytes, void* stream);
+size_t fg_beam_select_workspace_bytes(const fg_model_cfg* cfg, int32_t n_groups, int32_t beams, int32_t n_best);
+
+/* fg_beam_reorder_paged: the caches of all l layers (host array of l pools of one format and page count) behind the
+ * beams that were chosen: row i takes over the state of row parents[i] of its group (0 .. beams-1; anything else: its
+ * own), i.e. table_out[i] = table_in[parent], pos_out[i] = pos_in[parent] (rows cached), entries past the pages held are -1.
+ * Full pages are shared, not copied.  The page where row i's next position goes (slot pos/64) becomes row i's alone:
+ * if it is partly filled, the first row of the group that holds it keeps it and the others take a free page and a copy
+ * of its filled rows (up to the next multiple of 16) in every layer; if it is not begun, every row takes a free page.
+ * Group g owns pages g*pages_per_group .. (g+1)*pages_per_group - 1 of the pools (all below n_pages); free are those
+ * that no row of the group holds any more, and the lowest is taken first.  Pages outside the group's range (a prompt
+ * shared between groups) are only read: a row whose partly filled page lies there takes a copy.  A row that finds no
+ * free page, or whose next position is beyond the table, gets no entry there (-1: appending skips it) and counts in
+ * missing[g] (int32 per group, or NULL).  pages_per_group = pages of the prompt + beams * (own pages per beam + 1)
+ * always suffices.
+ * table_in, pos_in, parents, table_out [rows][table_stride], pos_out: device int32, rows = n_groups * beams; table_out
+ * may be table_in and pos_out pos_in, other overlaps are not allowed.  ws >= fg_beam_reorder_workspace_bytes. */
+int fg_beam_reorder_paged(const fg_model_cfg* cfg, int32_t l, const fg_kv_pages* pages, int32_t n_groups, int32_t beams,
+                          int32_t pages_per_group, const int32_t* parents, const int32_t* table_in,
+                          const int32_t* pos_in, int32_t table_stride, int32_t* table_out, int32_t* pos_out,
+                          int32_t* missing, void* ws, size_t ws_bytes, void* stream);
+size_t fg_beam_reorder_workspace_bytes(int32_t n_groups, int32_t beams);
+
 /* ---- Per-kernel timing (HIP events on the caller's stream) -----------------------------
  * Between fg_profile_begin and fg_profile_end every kernel launch of the library is bracketed
  * by two events.  fg_profile_end synchronises and accumulates, per kernel class, the summed
@@ -379,10 +449,12 @@ int64_t fg_diagonal_pages_needed(int32_t n_seqs, int32_t s, int32_t n, int32_t g
  * Classes: GEMM_SMALL_M = projections in the decode shape (up to 320 rows on tiled 4-bit or FP16
  * weights, up to 512 otherwise) and GEMM_SMALL_M_FINISH their partial-sum reduction pass;
  * GEMM_LARGE_M = projections in the prefill shape (reduction pass included);
- * ATTN_DECODE covers the dense and the Top-K decode attention. */
+ * ATTN_DECODE covers the dense, the Top-K and the shared-page decode attention; BEAM_SELECT and BEAM_REORDER both
+ * launches of their calls. */
 typedef enum {
   FG_K_QUANTIZE = 0, FG_K_DEQUANTIZE, FG_K_LAYERNORM, FG_K_GEMM_SMALL_M, FG_K_GEMM_SMALL_M_FINISH,
   FG_K_GEMM_LARGE_M, FG_K_KV_APPEND, FG_K_ATTN_DECODE, FG_K_ATTN_PREFILL, FG_K_EMBED, FG_K_ARGMAX,
+  FG_K_KV_GATHER, FG_K_BEAM_SELECT, FG_K_BEAM_REORDER,
   FG_K_COUNT
 } fg_kernel_class;
 int fg_profile_begin(void);

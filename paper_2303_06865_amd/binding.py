@@ -14,9 +14,10 @@ import torch
 
 FG_OK = 0
 FG_ERR_NULL, FG_ERR_SHAPE, FG_ERR_UNSUPPORTED, FG_ERR_WORKSPACE, FG_ERR_DEVICE = -1, -2, -3, -4, -5
-FG_F16, FG_Q4G64, FG_Q4G64_TILED, FG_Q4G64_H16, FG_Q4G64_H16_TILED = 0, 1, 2, 3, 4
+FG_F16, FG_Q4G64, FG_Q4G64_TILED, FG_Q4G64_H16, FG_Q4G64_H16_TILED, FG_I8P64 = 0, 1, 2, 3, 4, 5
+FG_MAX_BEAMS, FG_MAX_BEST = 16, 32
 KERNEL_CLASSES = ["quantize", "dequantize", "layernorm", "gemm_small_m", "gemm_small_m_finish", "gemm_large_m",
-                  "kv_append", "attn_decode", "attn_prefill", "embed", "argmax"]
+                  "kv_append", "attn_decode", "attn_prefill", "embed", "argmax", "kv_gather", "beam_select", "beam_reorder"]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libfg.so")
@@ -112,6 +113,21 @@ EXPORTS = {
     "fg_decode_attention_paged": (C.c_int, [C.POINTER(fg_model_cfg), C.c_void_p, C.c_int64, C.c_int32,
                                             C.POINTER(fg_kv_pages), C.POINTER(fg_ragged), C.c_int32, C.c_void_p,
                                             C.c_void_p]),
+    "fg_decode_attention_beams_paged": (C.c_int, [C.POINTER(fg_model_cfg), C.c_int32, C.c_int32, C.c_void_p, C.c_int64,
+                                                  C.c_int32, C.POINTER(fg_kv_pages), C.POINTER(fg_ragged), C.c_int32,
+                                                  C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "fg_decode_attention_beams_workspace_bytes": (C.c_size_t, [C.POINTER(fg_model_cfg), C.c_int32, C.c_int32, C.c_int32,
+                                                               C.c_int32]),
+    "fg_kv_gather_paged": (C.c_int, [C.POINTER(fg_model_cfg), C.POINTER(fg_kv_pages), C.POINTER(fg_ragged), C.c_int32,
+                                     C.c_int32, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]),
+    "fg_beam_select": (C.c_int, [C.POINTER(fg_model_cfg), C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_int64,
+                                 C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                 C.c_void_p, C.c_size_t, C.c_void_p]),
+    "fg_beam_select_workspace_bytes": (C.c_size_t, [C.POINTER(fg_model_cfg), C.c_int32, C.c_int32, C.c_int32]),
+    "fg_beam_reorder_paged": (C.c_int, [C.POINTER(fg_model_cfg), C.c_int32, C.POINTER(fg_kv_pages), C.c_int32, C.c_int32,
+                                        C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p,
+                                        C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "fg_beam_reorder_workspace_bytes": (C.c_size_t, [C.c_int32, C.c_int32]),
     "fg_decode_layer_paged": (C.c_int, [C.POINTER(fg_model_cfg), C.POINTER(fg_layer_weights), C.c_void_p, C.c_int32,
                                         C.c_int32, C.POINTER(fg_kv_pages), C.POINTER(fg_ragged), C.c_void_p, C.c_void_p,
                                         C.c_size_t, C.c_void_p]),
@@ -287,11 +303,21 @@ class KVPages:
     [n_pages, nh, 64, dh/64, 2] {min, scale} pairs (binary32, or FP16 with meta_f16)."""
 
     def __init__(self, cfg: Cfg, n_pages: int, meta_f16: bool = False, device="cuda", zero: bool = True,
-                 quantized: bool = True):
-        """quantized = False: the pages hold plain FP16 rows [n_pages, nh, 64, dh] (FG_F16)."""
-        self.n_pages, self.meta_f16, self.quantized = n_pages, bool(meta_f16 and quantized), quantized
+                 quantized: bool = True, int8: bool = False):
+        """quantized = False: the pages hold plain FP16 rows [n_pages, nh, 64, dh] (FG_F16).
+        int8: 8-bit codes (FG_I8P64), keys [n_pages, nh, 64, dh], values [n_pages, nh, 4, dh, 16] (16 positions of
+        one head dimension next to each other), one binary32 scale per page and head [n_pages, nh]."""
+        self.n_pages, self.meta_f16, self.quantized = n_pages, bool(meta_f16 and quantized and not int8), quantized
+        self.int8 = int8
         mk = torch.zeros if zero else torch.empty
         nh, dh = cfg.nh, cfg.dh
+        if int8:
+            self.k_codes = mk((n_pages, nh, PAGE_ROWS, dh), dtype=torch.int8, device=device)
+            self.v_codes = mk((n_pages, nh, PAGE_ROWS // 16, dh, 16), dtype=torch.int8, device=device)
+            self.k_meta = mk((n_pages, nh), dtype=torch.float32, device=device)
+            self.v_meta = mk((n_pages, nh), dtype=torch.float32, device=device)
+            self.c = fg_kv_pages(_p(self.k_codes), _p(self.k_meta), _p(self.v_codes), _p(self.v_meta), FG_I8P64, n_pages)
+            return
         if not quantized:
             self.k_codes = mk((n_pages, nh, PAGE_ROWS, dh), dtype=torch.float16, device=device)
             self.v_codes = mk((n_pages, nh, PAGE_ROWS, dh), dtype=torch.float16, device=device)
@@ -305,6 +331,22 @@ class KVPages:
         self.v_meta = mk((n_pages, nh, PAGE_ROWS, dh // 64, 2), dtype=mt, device=device)
         self.c = fg_kv_pages(_p(self.k_codes), _p(self.k_meta), _p(self.v_codes), _p(self.v_meta),
                              FG_Q4G64_H16 if meta_f16 else FG_Q4G64, n_pages)
+
+    @staticmethod
+    def of(k_codes: torch.Tensor, k_meta: Optional[torch.Tensor], v_codes: torch.Tensor, v_meta: Optional[torch.Tensor],
+           dtype: int) -> "KVPages":
+        """A pool over tensors that the caller made, in the shapes above (e.g. one layer of a tensor that holds all)."""
+        for t in (k_codes, k_meta, v_codes, v_meta):
+            assert t is None or (t.is_cuda and t.is_contiguous() and t.shape[:2] == k_codes.shape[:2])
+        assert k_codes.numel() == v_codes.numel() and k_codes.dtype == v_codes.dtype
+        assert k_codes.dtype == {FG_F16: torch.float16, FG_I8P64: torch.int8}.get(dtype, torch.uint8)
+        assert (k_meta is None) == (v_meta is None) == (dtype == FG_F16)
+        assert k_meta is None or k_meta.dtype == v_meta.dtype == (torch.float16 if dtype == FG_Q4G64_H16 else torch.float32)
+        p = KVPages.__new__(KVPages)
+        p.n_pages, p.meta_f16, p.quantized, p.int8 = k_codes.shape[0], dtype == FG_Q4G64_H16, dtype != FG_F16, dtype == FG_I8P64
+        p.k_codes, p.k_meta, p.v_codes, p.v_meta = k_codes, k_meta, v_codes, v_meta
+        p.c = fg_kv_pages(_p(k_codes), _p(k_meta), _p(v_codes), _p(v_meta), dtype, p.n_pages)
+        return p
 
     def nbytes(self) -> int:
         n = 2 * self.k_codes.numel() * self.k_codes.element_size()
@@ -471,6 +513,90 @@ def fg_decode_attention_paged(cfg: Cfg, q: torch.Tensor, q_row_stride: int, b: i
     _check(lib().fg_decode_attention_paged(C.byref(cfg.c), _p(q), q_row_stride, b, C.byref(pages.c), C.byref(seqs.c),
                                            rows_bias, _p(out), _stream()), "fg_decode_attention_paged")
     return out
+
+
+def decode_attention_beams_workspace(cfg: Cfg, nkv: int, beams: int, b: int, table_stride: int) -> torch.Tensor:
+    return _ws(lib().fg_decode_attention_beams_workspace_bytes(C.byref(cfg.c), nkv, beams, b, table_stride))
+
+
+def fg_decode_attention_beams_paged(cfg: Cfg, nkv: int, beams: int, q: torch.Tensor, q_row_stride: int, b: int,
+                                    pages: KVPages, seqs: Ragged, rows_bias: int = 0, ws: Optional[torch.Tensor] = None,
+                                    out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of b rows over 8-bit pages of nkv heads; each `beams` rows in turn share the pages that their tables share."""
+    if out is None:
+        out = torch.empty((b, cfg.h1), dtype=torch.float16, device=q.device)
+    if ws is None:
+        ws = decode_attention_beams_workspace(cfg, nkv, beams, b, seqs.page_table.shape[1])
+    _check(lib().fg_decode_attention_beams_paged(C.byref(cfg.c), nkv, beams, _p(q), q_row_stride, b, C.byref(pages.c),
+                                                 C.byref(seqs.c), rows_bias, _p(out), _p(ws), ws.numel(), _stream()),
+           "fg_decode_attention_beams_paged")
+    return out
+
+
+def fg_kv_gather_paged(cfg: Cfg, pages: KVPages, seqs: Ragged, b: int, s: int, k_out: Optional[torch.Tensor] = None,
+                       v_out: Optional[torch.Tensor] = None, row_stride: Optional[int] = None):
+    """Positions pos[i] .. pos[i] + s - 1 of sequence seq_ids[i] as FP16 (k, v), [b, s, h1]."""
+    if k_out is None:
+        k_out = torch.empty((b, s, cfg.h1), dtype=torch.float16, device=pages.k_codes.device)
+        v_out = torch.empty_like(k_out)
+        row_stride = cfg.h1
+    _check(lib().fg_kv_gather_paged(C.byref(cfg.c), C.byref(pages.c), C.byref(seqs.c), b, s, _p(k_out), _p(v_out),
+                                    row_stride, _stream()), "fg_kv_gather_paged")
+    return k_out, v_out
+
+
+def beam_select_workspace(cfg: Cfg, n_groups: int, beams: int, n_best: int) -> torch.Tensor:
+    return _ws(lib().fg_beam_select_workspace_bytes(C.byref(cfg.c), n_groups, beams, n_best))
+
+
+def fg_beam_select(cfg: Cfg, logits: torch.Tensor, scores: torch.Tensor, beams: int, n_best: Optional[int] = None,
+                   done: Optional[torch.Tensor] = None, eos: int = -1, ws: Optional[torch.Tensor] = None):
+    """logits float32 [n * beams, vocab] (rows may be apart), scores float32 [n * beams], done int32 [n * beams] or None.
+    Returns (beams int32, ids int32, scores float32, done int32), each [n, n_best], best first."""
+    assert logits.dtype == torch.float32 and logits.is_cuda and logits.dim() == 2 and logits.stride(1) == 1
+    assert logits.shape[1] == cfg.vocab
+    rows = logits.shape[0]
+    assert scores.dtype == torch.float32 and scores.is_cuda and scores.is_contiguous() and scores.numel() == rows
+    assert done is None or (done.dtype == torch.int32 and done.is_cuda and done.is_contiguous() and done.numel() == rows)
+    assert rows % beams == 0
+    n_best = beams if n_best is None else n_best
+    n = rows // beams
+    ints = torch.empty((3, n, n_best), dtype=torch.int32, device=logits.device)
+    out = torch.empty((n, n_best), dtype=torch.float32, device=logits.device)
+    if ws is None:
+        ws = beam_select_workspace(cfg, n, beams, n_best)
+    _check(lib().fg_beam_select(C.byref(cfg.c), n, beams, n_best, _p(logits), max(logits.stride(0), cfg.vocab), _p(scores),
+                                _p(done), eos, _p(ints[0]), _p(ints[1]), _p(out), _p(ints[2]), _p(ws), ws.numel(), _stream()),
+           "fg_beam_select")
+    return ints[0], ints[1], out, ints[2]
+
+
+def beam_reorder_workspace(n_groups: int, beams: int) -> torch.Tensor:
+    return _ws(lib().fg_beam_reorder_workspace_bytes(n_groups, beams))
+
+
+def fg_beam_reorder_paged(cfg: Cfg, pages: Sequence[KVPages], table: torch.Tensor, pos: torch.Tensor, parents: torch.Tensor,
+                          beams: int, pages_per_group: int, ws: Optional[torch.Tensor] = None,
+                          table_out: Optional[torch.Tensor] = None, pos_out: Optional[torch.Tensor] = None,
+                          missing: Optional[torch.Tensor] = None):
+    """table int32 [n * beams, table_stride], pos and parents int32 [n * beams]; pages: one pool per layer.  Returns
+    (table, pos, missing int32 [n]); table_out = table and pos_out = pos rewrite them in place."""
+    rows, stride = table.shape
+    for t in (table, pos, parents, table_out, pos_out, missing):
+        assert t is None or (t.dtype == torch.int32 and t.is_cuda and t.is_contiguous())
+    assert pos.numel() == rows and parents.numel() == rows and rows % beams == 0
+    table_out = torch.empty_like(table) if table_out is None else table_out
+    pos_out = torch.empty_like(pos) if pos_out is None else pos_out
+    assert table_out.shape == table.shape and pos_out.numel() == rows
+    if missing is None:
+        missing = torch.empty((rows // beams,), dtype=torch.int32, device=table.device)
+    if ws is None:
+        ws = beam_reorder_workspace(rows // beams, beams)
+    parr = (fg_kv_pages * len(pages))(*[p.c for p in pages])
+    _check(lib().fg_beam_reorder_paged(C.byref(cfg.c), len(pages), parr, rows // beams, beams, pages_per_group, _p(parents),
+                                       _p(table), _p(pos), stride, _p(table_out), _p(pos_out), _p(missing), _p(ws),
+                                       ws.numel(), _stream()), "fg_beam_reorder_paged")
+    return table_out, pos_out, missing
 
 
 def fg_decode_attention_topk_paged(cfg: Cfg, q: torch.Tensor, q_row_stride: int, b: int, topk: int, pages: KVPages,

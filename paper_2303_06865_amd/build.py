@@ -25,6 +25,9 @@ SOURCES = [
     "fg_attn_decode.hip",
     "fg_attn_topk.hip",
     "fg_attn_prefill.hip",
+    "fg_kv_i8.hip",
+    "fg_attn_i8.hip",
+    "fg_beam.hip",
     "fg_layer.hip",
 ]
 
@@ -34,8 +37,9 @@ COMMON = [
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wno-unused-command-line-argument",
 ]
-# the quantizer must be a bit-exact function of its input: no fused multiply-add, IEEE division
-PER_FILE = {"fg_quant.hip": ["-ffp-contract=off", "-fhip-fp32-correctly-rounded-divide-sqrt"]}
+# the quantizers must be bit-exact functions of their inputs: no fused multiply-add, IEEE division
+PER_FILE = {"fg_quant.hip": ["-ffp-contract=off", "-fhip-fp32-correctly-rounded-divide-sqrt"],
+            "fg_kv_i8.hip": ["-ffp-contract=off", "-fhip-fp32-correctly-rounded-divide-sqrt"]}
 
 
 def _hipcc() -> str:

@@ -650,6 +650,8 @@ int decode_attention_paged_launch(const fg_model_cfg& cfg, const half_t* q, int6
                                   const fg_kv_pages& pages, const fg_ragged& seqs, int32_t rows_bias, half_t* out,
                                   hipStream_t stream) {
   if (b == 0) return FG_OK;
+  if (pages.dtype == FG_I8P64)
+    return decode_attention_i8_launch(cfg, cfg.nh, 1, q, q_stride, b, pages, seqs, rows_bias, out, nullptr, 0, stream);
   const int dh = cfg.h1 / cfg.nh;
   AttnArgs a;
   a.q = q;

@@ -96,13 +96,15 @@ int check_pages(const fg_model_cfg* cfg, const fg_kv_pages* pages, const fg_ragg
   (void)cfg;
   if (!pages || !seqs) return FG_ERR_NULL;
   const bool q4 = pages->dtype == FG_Q4G64 || pages->dtype == FG_Q4G64_H16;
-  if (!q4 && pages->dtype != FG_F16) return FG_ERR_UNSUPPORTED;
+  const bool i8 = pages->dtype == FG_I8P64;
+  if (!q4 && !i8 && pages->dtype != FG_F16) return FG_ERR_UNSUPPORTED;
   if (pages->n_pages <= 0 || seqs->table_stride <= 0 || seqs->n_seqs <= 0) return FG_ERR_SHAPE;
   if ((int64_t)seqs->table_stride * FG_PAGE_ROWS > 0x7fffffff) return FG_ERR_SHAPE;
   if (!pages->k_codes || !pages->v_codes || !seqs->page_table) return FG_ERR_NULL;
-  if (q4 && (!pages->k_meta || !pages->v_meta)) return FG_ERR_NULL;
+  if ((q4 || i8) && (!pages->k_meta || !pages->v_meta)) return FG_ERR_NULL;
   if (!aligned16(pages->k_codes) || !aligned16(pages->v_codes)) return FG_ERR_SHAPE;
   if (q4 && (!aligned16(pages->k_meta) || !aligned16(pages->v_meta))) return FG_ERR_SHAPE;
+  if (i8 && ((reinterpret_cast<uintptr_t>(pages->k_meta) | reinterpret_cast<uintptr_t>(pages->v_meta)) & 3u)) return FG_ERR_SHAPE;
   return FG_OK;
 }
 
@@ -282,6 +284,9 @@ static int run_layer(const fg_model_cfg& c, const fg_layer_weights& w, const hal
       if (topk > 0)
         rc = decode_attention_topk_paged_launch(c, L.qkv, 3 * h1, b, topk, *paged->pages, *paged->seqs, 1, L.o,
                                                 nullptr, st);
+      else if (paged->pages->dtype == FG_I8P64)   // the buffers from act on are free here
+        rc = decode_attention_i8_launch(c, c.nh, 1, L.qkv, 3 * h1, b, *paged->pages, *paged->seqs, 1, L.o, L.act,
+                                        L.total - (reinterpret_cast<unsigned char*>(L.act) - reinterpret_cast<unsigned char*>(ws)), st);
       else
         rc = decode_attention_paged_launch(c, L.qkv, 3 * h1, b, *paged->pages, *paged->seqs, 1, L.o, st);
       if (rc) return rc;
@@ -365,7 +370,7 @@ extern "C" const char* fg_error_string(int status) {
     case FG_OK: return "ok";
     case FG_ERR_NULL: return "a required pointer is NULL";
     case FG_ERR_SHAPE: return "bad shape, size or alignment";
-    case FG_ERR_UNSUPPORTED: return "unsupported format (only 4-bit codes, groups of 64, head size 64 or 128)";
+    case FG_ERR_UNSUPPORTED: return "unsupported format (only 4-bit codes in groups of 64, 8-bit cache pages, head size 64 or 128)";
     case FG_ERR_WORKSPACE: return "workspace missing or too small";
     case FG_ERR_DEVICE: return "HIP runtime error";
   }
@@ -379,7 +384,8 @@ extern "C" int fg_version(void) { return 100; }
 extern "C" const char* fg_kernel_class_name(int k) {
   static const char* names[FG_K_COUNT] = {"quantize",      "dequantize",          "layernorm",    "gemm_small_m",
                                           "gemm_small_m_finish", "gemm_large_m",  "kv_append",    "attn_decode",
-                                          "attn_prefill",  "embed",               "argmax"};
+                                          "attn_prefill",  "embed",               "argmax",
+                                          "kv_gather",     "beam_select",         "beam_reorder"};
   return (k >= 0 && k < FG_K_COUNT) ? names[k] : "?";
 }
 
@@ -939,10 +945,10 @@ extern "C" int fg_generate_diagonal(const fg_model_cfg* cfg, int32_t l, const fg
   const int gbs = gpu_batch_size;
   for (int j = 0; j < l; ++j) {
     if ((rc = check_layer(cfg, &layers[j]))) return rc;
-    const bool q4 = pages[j].dtype == FG_Q4G64 || pages[j].dtype == FG_Q4G64_H16;
-    if (!q4 && pages[j].dtype != FG_F16) return FG_ERR_UNSUPPORTED;
+    const bool coded = pages[j].dtype == FG_Q4G64 || pages[j].dtype == FG_Q4G64_H16 || pages[j].dtype == FG_I8P64;
+    if (!coded && pages[j].dtype != FG_F16) return FG_ERR_UNSUPPORTED;
     if (pages[j].n_pages != pages[0].n_pages || pages[j].n_pages <= 0) return FG_ERR_SHAPE;
-    if (!pages[j].k_codes || !pages[j].v_codes || (q4 && (!pages[j].k_meta || !pages[j].v_meta))) return FG_ERR_NULL;
+    if (!pages[j].k_codes || !pages[j].v_codes || (coded && (!pages[j].k_meta || !pages[j].v_meta))) return FG_ERR_NULL;
     if (layers[j].wqkv.dtype != layers[0].wqkv.dtype || layers[j].wo.dtype != layers[0].wo.dtype ||
         layers[j].w1.dtype != layers[0].w1.dtype || layers[j].w2.dtype != layers[0].w2.dtype)
       return FG_ERR_UNSUPPORTED;

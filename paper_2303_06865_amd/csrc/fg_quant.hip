@@ -243,6 +243,7 @@ int kv_append_paged_launch(const fg_model_cfg& cfg, const half_t* k, const half_
                            int32_t b, int32_t s, const fg_kv_pages& pages, const fg_ragged& seqs, bool use_pos,
                            hipStream_t stream) {
   if (b == 0 || s == 0) return FG_OK;
+  if (pages.dtype == FG_I8P64) return kv_append_i8_launch(cfg, k, v, row_stride, b, s, pages, seqs, use_pos, stream);
   KvAppendArgs a;
   a.src[0] = k;
   a.src[1] = v;
