@@ -1,9 +1,33 @@
-// Decode attention over 8-bit pages (FG_I8P64): softmax(q K^T / sqrt(dh)) V for one token per row.
+// Decode attention over 8-bit pages (FG_I8P64): softmax(q K^T / sqrt(dh)) V for one token per row, several rows and query
+// heads on the same keys and values at once.
+//
+// Both products run on the integer matrix cores, on the stored codes as they are: no code is ever unpacked.  What stands on
+// the other side is a number in four digits of seven bits:
+//   q_d = (max |q| / C) * sum_t 2^(7t) a_td,   |a_td| <= 127,   C = 2^28 - 64     (signs in every digit)
+//   p_j =             1 / C  * sum_t 2^(7t) b_tj,  0 <= b_tj <= 127               (p = 2^(s - max over the page) <= 1)
+// so that q.k = (max|q| / C) S_k sum_t 2^(7t) (a_t . c) with exact 32-bit integer sums, put together in binary32.  Queries are
+// off by 2^-29 of their largest element, weights by 2^-28 of the page's largest: both below what binary32 sums lose.  The four
+// digits are four columns of v_mfma_i32_16x16x64_i8; its sixteen columns are four queries: the beams of a sequence that share
+// the page, or the query heads of a cache head, or (one query) idle, at no cost, because the loads are what bounds this.
+//
+//   S^T[key][column] = K . A^T    rows = keys; row m of block i is key 16 (m / 4) + 4 i + m % 4 of the page, so that lane
+//                                 group g (lane / 16) ends up with keys 16 g .. 16 g + 15, four per block
+//   O^T[d][column] += V^T . B^T   the lane group's 16 weights, packed to bytes, are the operand already; the pages hold the
+//                                 value codes of 16 positions next to each other, which is the other operand
+//
+// A unit is (group of rows, cache head, up to 4 NT queries); WPU waves share a unit's pages round-robin, and SPLITS workgroups
+// where the units are too few for the chip.  Each keeps a running (maximum, sum, output) per column; they are merged through
+// LDS, and through memory by a second launch where there are splits.  A wave has the values of a page and the keys of its next
+// one on their way while it computes.
 #include "fg_attn_common.h"
 
 namespace fg {
 
 namespace {
+
+typedef int i4_t __attribute__((ext_vector_type(4)));
+
+constexpr float kDigits = 268435392.0f;   // C = 2^28 - 64: max|q| * (C / max|q|), off by two roundings, stays below 2^28
 
 struct AttnI8Args {
   const half_t* q;
@@ -16,69 +40,385 @@ struct AttnI8Args {
   const int32_t* page_table;   // [n_seqs][table_stride]
   const int32_t* seq_ids;      // [b] or nullptr
   const int32_t* seq_rows;     // [b]: rows attended = seq_rows[i] + rows_bias
-  int b, nh, nkv;
+  int nh, nkv, beams;
+  int n_units, chunks;         // units = groups * nkv * chunks
   int table_stride, n_seqs, n_pages, rows_bias;
   float scale;
+  int splits;
+  float2* part_ml;             // [b * nh][splits]: maximum (log2 units) and sum
+  float* part_o;               // [b * nh][splits][dh]
 };
 
-// One wave per (row, query head).  Scores: lane = position of the page; output: lane = head dimension(s).
-template <int DH>
-__global__ __launch_bounds__(64) void attn_decode_i8_kernel(AttnI8Args a) {
-  constexpr int ND = DH / 64;
-  __shared__ float sm_q[DH], sm_p[64];
-  const int lane = threadIdx.x;
-  const int row = blockIdx.x / a.nh, head = blockIdx.x - row * a.nh, kv = head / (a.nh / a.nkv);
-  int sid = a.seq_ids ? a.seq_ids[row] : row;
-  sid = sid < 0 ? 0 : (sid >= a.n_seqs ? a.n_seqs - 1 : sid);
-  const int32_t* tbl = a.page_table + (int64_t)sid * a.table_stride;
-  int64_t n = (int64_t)a.seq_rows[row] + a.rows_bias;
-  const int64_t most = (int64_t)a.table_stride * FG_PAGE_ROWS;
-  n = n < 0 ? 0 : (n > most ? most : n);
-  for (int d = lane; d < DH; d += 64) sm_q[d] = (float)a.q[(int64_t)row * a.q_stride + (int64_t)head * DH + d];
-  __syncthreads();
-  float m = -INFINITY, l = 0.f, o[ND] = {};
-  for (int64_t r0 = 0; r0 < n; r0 += FG_PAGE_ROWS) {
-    int pg = tbl[r0 >> 6];
-    pg = pg < 0 ? 0 : (pg >= a.n_pages ? a.n_pages - 1 : pg);
-    const int64_t ph = (int64_t)pg * a.nkv + kv;
-    const int8_t* kc = a.k_codes + (ph * FG_PAGE_ROWS + lane) * DH;
-    float s = 0.f;
-    for (int d = 0; d < DH; ++d) s += sm_q[d] * (float)kc[d];
-    s = r0 + lane < n ? s * a.k_scales[ph] * a.scale : -INFINITY;
-    const float m_new = fmaxf(m, wave_max(s));
-    const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - m_new) * kLog2e);
-    m = m_new;
-    const float p = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((s - m) * kLog2e);
-    l = l * alpha + p;
+__device__ __forceinline__ int seq_of(const AttnI8Args& a, int row) {
+  const int sid = a.seq_ids ? a.seq_ids[row] : row;
+  return sid < 0 ? 0 : (sid >= a.n_seqs ? a.n_seqs - 1 : sid);
+}
+__device__ __forceinline__ int rows_of(const AttnI8Args& a, int row) {
+  const int64_t n = (int64_t)a.seq_rows[row] + a.rows_bias, most = (int64_t)a.table_stride * FG_PAGE_ROWS;
+  return (int)(n < 0 ? 0 : (n > most ? most : n));
+}
+// The same bits in the four lanes: each takes its own digit of what comes of it.  (A product that the compiler fused into the
+// first addition would be rounded in one lane and not in the other.)
+__device__ __forceinline__ float quad_sum(float v) {
+  __asm__("" : "+v"(v));
+  v += dpp_f32<kDppXor1>(v);
+  return v + dpp_f32<kDppXor2>(v);
+}
+
+template <int DH, int NT, int WPU, bool SHARED>
+__global__ __launch_bounds__(256) void attn_decode_i8_kernel(AttnI8Args a) {
+  constexpr int KS = DH / 64;   // steps of 64 over the head size
+  constexpr int ND = DH / 16;   // blocks of 16 output rows
+  constexpr int UPB = 4 / WPU;  // units per workgroup
+  extern __shared__ uint2 sm_list[];   // SHARED: [wave][64 * beams] pages to visit: {page, slot in the window | beams << 8}
+  __shared__ float sm_m[4][4], sm_l[4][4];
+  __shared__ float sm_o[4][4][DH];
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int part = wave % WPU;
+  const int unit0 = blockIdx.x * UPB;
+  const bool there = unit0 + wave / WPU < a.n_units;
+  const int unit = there ? unit0 + wave / WPU : unit0;   // surplus waves of the last workgroup redo its first unit
+  const int chunk = unit % a.chunks, gh = unit / a.chunks;
+  const int kv = gh % a.nkv, group = gh / a.nkv;
+  const int col = lane & 15, g = lane >> 4, dig = col & 3;
+  const int per_kv = a.nh / a.nkv, nq = per_kv * a.beams, q_lo = chunk * 4 * NT;
+  const int split = blockIdx.y;
+
+  // ---- the lane's query of every tile: its digits, its number of rows
+  i4_t qop[NT][KS];
+  float qmul[NT];
+  int n_of[NT], beam_of[NT];
+  int n_max = 0;
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const int qi = q_lo + 4 * t + (col >> 2);
+    const bool valid = qi < nq;
+    const int qc = valid ? qi : nq - 1;
+    const int beam = qc / per_kv, row = group * a.beams + beam;
+    const half_t* src = a.q + (int64_t)row * a.q_stride + (int64_t)(kv * per_kv + qc % per_kv) * DH + 16 * g;
+    h8_t x[KS][2];
+    float top = 0.f;
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        x[k][h] = *reinterpret_cast<const h8_t*>(src + 64 * k + 8 * h);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf((float)x[k][h][e]));
+      }
+    top = xor32_reduce(xor16_reduce(top, OpMax()), OpMax());
+    const float inv = top > 0.f ? kDigits / top : 0.f;
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        uint32_t word = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float f = (float)x[k][w >> 1][4 * (w & 1) + e] * inv;
+          const int mag = (((int)rintf(fabsf(f)) >> (7 * dig)) & 127);
+          word |= (uint32_t)((f < 0.f ? -mag : mag) & 255) << (8 * e);
+        }
+        qop[t][k][w] = (int)word;
+      }
+    // scores come out in log2 units; the digit's weight goes in here
+    qmul[t] = top * (a.scale * kLog2e / kDigits) * (float)(1 << (7 * dig));
+    const int n = rows_of(a, row);
+    n_of[t] = valid ? n : 0x7fffffff;   // an idle column is never masked, and never written
+    beam_of[t] = beam;
+    n_max = max(n_max, n);
+  }
+  n_max = __builtin_amdgcn_readfirstlane((int)wave_max((float)((n_max + 63) >> 6)));   // pages: exact in binary32
+  const int per_split = (n_max + a.splits - 1) / a.splits;
+  const int s_lo = split * per_split, s_hi = min(n_max, s_lo + per_split);
+
+  float m_run[NT], l_run[NT];
+  f4_t o[NT][ND];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    m_run[t] = -INFINITY;
+    l_run[t] = 0.f;
+#pragma unroll
+    for (int j = 0; j < ND; ++j) o[t][j] = (f4_t){0.f, 0.f, 0.f, 0.f};
+  }
+
+  i4_t kreg[4][KS], vreg[ND];
+  const int64_t page_bytes = FG_PAGE_ROWS * DH;
+  const int k_at = (16 * (col >> 2) + (col & 3)) * DH + 16 * g, v_at = (g * DH + col) * 16;
+  auto load_k = [&](int page) {
+    const int8_t* p = a.k_codes + ((int64_t)page * a.nkv + kv) * page_bytes + k_at;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int k = 0; k < KS; ++k) kreg[i][k] = *reinterpret_cast<const i4_t*>(p + 4 * i * DH + 64 * k);
+  };
+  auto load_v = [&](int page) {
+    const int8_t* p = a.v_codes + ((int64_t)page * a.nkv + kv) * page_bytes + v_at;
+#pragma unroll
+    for (int j = 0; j < ND; ++j) vreg[j] = *reinterpret_cast<const i4_t*>(p + 256 * j);
+  };
+
+  const int b_lo = q_lo / per_kv, b_hi = min(nq - 1, q_lo + 4 * NT - 1) / per_kv;   // beams of this unit
+  const int32_t* tbl0 = a.page_table + (int64_t)seq_of(a, group * a.beams + b_lo) * a.table_stride;
+  uint2* list = sm_list + wave * 64 * a.beams;
+  auto clamp_page = [&](int pg) { return pg < 0 ? 0 : (pg >= a.n_pages ? a.n_pages - 1 : pg); };
+
+  for (int w0 = s_lo + part; w0 < s_hi; w0 += 64 * WPU) {   // windows of 64 of this wave's slots
+    const int slot_l = w0 + WPU * lane;
+    const bool in = slot_l < s_hi;
+    int count, pages = 0;
+    if constexpr (SHARED) {
+      // every page once, with the beams that name it; in the order of the beams, then of the slots
+      int e[FG_MAX_BEAMS];
+#pragma unroll
+      for (int k = 0; k < FG_MAX_BEAMS; ++k) {
+        e[k] = -1;
+        if (k <= b_hi - b_lo) {
+          const int row = group * a.beams + b_lo + k;
+          if (in && rows_of(a, row) > (slot_l << 6))
+            e[k] = clamp_page(a.page_table[(int64_t)seq_of(a, row) * a.table_stride + slot_l]);
+        }
+      }
+      count = 0;
+#pragma unroll
+      for (int k = 0; k < FG_MAX_BEAMS; ++k) {
+        if (k > b_hi - b_lo) break;
+        bool first = e[k] >= 0;
+#pragma unroll
+        for (int i = 0; i < k; ++i) first = first && e[i] != e[k];
+        uint32_t who = 0;
+#pragma unroll
+        for (int i = k; i < FG_MAX_BEAMS; ++i) who |= e[i] == e[k] ? 1u << i : 0u;
+        const uint64_t m = __builtin_amdgcn_ballot_w64(first);
+        const int at = count + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0u));
+        if (first) list[at] = make_uint2((uint32_t)e[k], (uint32_t)lane | who << 8);
+        count += __builtin_popcountll(m);
+      }
+      wave_lds_fence();
+    } else {
+      count = __builtin_popcountll(__builtin_amdgcn_ballot_w64(in));
+      pages = clamp_page(tbl0[in ? slot_l : w0]);
+    }
+    auto visit = [&](int v, int& page, int& slot, uint32_t& who) {
+      if constexpr (SHARED) {
+        const uint2 e = list[v];
+        page = __builtin_amdgcn_readfirstlane(e.x);
+        const uint32_t y = __builtin_amdgcn_readfirstlane(e.y);
+        slot = w0 + WPU * (int)(y & 255);
+        who = y >> 8;
+      } else {
+        page = __builtin_amdgcn_readlane(pages, v);
+        slot = w0 + WPU * v;
+        who = 1;
+      }
+    };
+
+    int page = 0, slot = 0;
+    uint32_t who = 0;
+    if (count > 0) {
+      visit(0, page, slot, who);
+      load_k(page);
+    }
+    for (int v = 0; v < count; ++v) {
+      const float ks = a.k_scales[(int64_t)page * a.nkv + kv], vs = a.v_scales[(int64_t)page * a.nkv + kv];
+      load_v(page);
+      int page_n = page, slot_n = slot;
+      uint32_t who_n = who;
+      if (v + 1 < count) visit(v + 1, page_n, slot_n, who_n);
+      __builtin_amdgcn_sched_barrier(0);
+      i4_t acc[NT][4];
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          acc[t][i] = (i4_t){0, 0, 0, 0};
+#pragma unroll
+          for (int k = 0; k < KS; ++k)
+            acc[t][i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(kreg[i][k], qop[t][k], acc[t][i], 0, 0, 0);
+        }
+      __builtin_amdgcn_sched_barrier(0);
+      if (v + 1 < count) load_k(page_n);
+      __builtin_amdgcn_sched_barrier(0);
+      const int left = slot << 6;
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const float f = qmul[t] * ks;
+        float s[4][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) s[i][r] = quad_sum((float)acc[t][i][r] * f);
+        const bool mine = !SHARED || (who >> (beam_of[t] - b_lo) & 1) || n_of[t] == 0x7fffffff;
+        if (__builtin_amdgcn_ballot_w64(!mine || left > n_of[t] - 64) != 0) {
+          const int n = mine ? n_of[t] - left - 16 * g : 0;   // keys of the lane's sixteen that count
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) s[i][r] = 4 * i + r < n ? s[i][r] : -INFINITY;
+        }
+        float top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) top = fmaxf(top, s[i][r]);
+        top = xor32_reduce(xor16_reduce(top, OpMax()), OpMax());
+        const float use = top == -INFINITY ? 0.f : top;
+        const float m_new = fmaxf(m_run[t], top), m_use = m_new == -INFINITY ? 0.f : m_new;
+        const float alpha = fast_exp2(m_run[t] - m_use), beta = fast_exp2(top - m_use);
+        m_run[t] = m_new;
+        float sum = 0.f;
+        i4_t pop;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          uint32_t d[4];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const float p = fast_exp2(s[i][r] - use);
+            sum += p;
+            d[r] = ((uint32_t)(p * kDigits) >> (7 * dig)) & 127u;
+          }
+          pop[i] = (int)(d[0] | d[1] << 8 | d[2] << 16 | d[3] << 24);
+        }
+        l_run[t] = l_run[t] * alpha + sum * beta;
+        if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
+#pragma unroll
+          for (int j = 0; j < ND; ++j) o[t][j] *= alpha;
+        }
+        const float bv = beta * vs;
+#pragma unroll
+        for (int j = 0; j < ND; ++j) {
+          const i4_t z = {0, 0, 0, 0};
+          const i4_t po = __builtin_amdgcn_mfma_i32_16x16x64_i8(vreg[j], pop, z, 0, 0, 0);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) o[t][j][r] = __builtin_fmaf((float)po[r], bv, o[t][j][r]);
+        }
+      }
+      page = page_n, slot = slot_n, who = who_n;
+    }
+    if constexpr (SHARED) wave_lds_fence();   // the list is read before it is written again
+  }
+
+  // ---- digits together, then waves, then (second launch) splits
+  const float wd = (float)(1 << (7 * dig)) / kDigits;
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const float l = xor32_reduce(xor16_reduce(l_run[t], OpAdd()), OpAdd());
+    f4_t x[ND];
+#pragma unroll
+    for (int j = 0; j < ND; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) x[j][r] = quad_sum(o[t][j][r] * wd);
+    const int qi = q_lo + 4 * t + (col >> 2);
+    if (WPU == 1 && a.splits == 1) {
+      if (qi < nq && there) {
+        const int row = group * a.beams + qi / per_kv, head = kv * per_kv + qi % per_kv;
+        const float inv = l > 0.f ? 1.0f / l : 0.f;   // no rows attended: zeros
+        half_t* dst = a.out + ((int64_t)row * a.nh + head) * DH + 4 * g;
+#pragma unroll
+        for (int j = 0; j < ND; ++j)
+          if ((j & 3) == dig) {
+            h4_t h;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) h[r] = (half_t)(x[j][r] * inv);
+            *reinterpret_cast<h4_t*>(dst + 16 * j) = h;
+          }
+      }
+      continue;
+    }
+    if (t > 0) __syncthreads();   // the tile before has been read
+    if (lane < 16 && dig == 0) {
+      sm_m[wave][col >> 2] = m_run[t];
+      sm_l[wave][col >> 2] = l;
+    }
+#pragma unroll
+    for (int j = 0; j < ND; ++j)
+      if ((j & 3) == dig) *reinterpret_cast<f4_t*>(&sm_o[wave][col >> 2][16 * j + 4 * g]) = x[j];
     __syncthreads();
-    sm_p[lane] = p * a.v_scales[ph];
-    __syncthreads();
-    const int8_t* vc = a.v_codes + ph * (FG_PAGE_ROWS * DH);
-    for (int j = 0; j < ND; ++j) {
-      float acc = 0.f;
-      for (int r = 0; r < FG_PAGE_ROWS; ++r) acc += sm_p[r] * (float)vc[((r >> 4) * DH + lane + 64 * j) * 16 + (r & 15)];
-      o[j] = o[j] * alpha + acc;
+    for (int i = tid; i < UPB * 4 * DH; i += 256) {
+      const int d = i % DH, qs = i / DH % 4, u = i / (4 * DH);
+      const int un = unit0 + u;
+      const int qn = un % a.chunks * 4 * NT + 4 * t + qs;
+      if (un >= a.n_units || qn >= nq) continue;
+      const int row = un / a.chunks / a.nkv * a.beams + qn / per_kv, head = un / a.chunks % a.nkv * per_kv + qn % per_kv;
+      float M = -INFINITY, num = 0.f, den = 0.f;
+#pragma unroll
+      for (int w = 0; w < WPU; ++w) M = fmaxf(M, sm_m[u * WPU + w][qs]);
+#pragma unroll
+      for (int w = 0; w < WPU; ++w) {
+        const float mw = sm_m[u * WPU + w][qs], fw = mw == -INFINITY ? 0.f : fast_exp2(mw - M);
+        num += fw * sm_o[u * WPU + w][qs][d];
+        den += fw * sm_l[u * WPU + w][qs];
+      }
+      const int64_t rh = (int64_t)row * a.nh + head;
+      if (a.splits == 1) {
+        a.out[rh * DH + d] = (half_t)(den > 0.f ? num / den : 0.f);
+      } else {
+        a.part_o[(rh * a.splits + split) * DH + d] = num;
+        if (d == 0) a.part_ml[rh * a.splits + split] = make_float2(M, den);
+      }
     }
   }
-  l = wave_sum(l);
-  for (int j = 0; j < ND; ++j)
-    a.out[((int64_t)row * a.nh + head) * DH + lane + 64 * j] = (half_t)(l > 0.f ? o[j] / l : 0.f);
+}
+
+// One wave per (row, query head): the splits' partial results together.
+template <int DH>
+__global__ __launch_bounds__(256) void attn_merge_i8_kernel(AttnI8Args a, int64_t n) {
+  const int lane = threadIdx.x & 63;
+  const int64_t rh = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (rh >= n) return;
+  const float2* ml = a.part_ml + rh * a.splits;
+  float M = -INFINITY;
+  for (int s = 0; s < a.splits; ++s) M = fmaxf(M, ml[s].x);
+  float den = 0.f, num[DH / 64] = {};
+  for (int s = 0; s < a.splits; ++s) {
+    const float f = ml[s].x == -INFINITY ? 0.f : fast_exp2(ml[s].x - M);
+    den += f * ml[s].y;
+#pragma unroll
+    for (int k = 0; k < DH / 64; ++k) num[k] += f * a.part_o[(rh * a.splits + s) * DH + lane + 64 * k];
+  }
+#pragma unroll
+  for (int k = 0; k < DH / 64; ++k) a.out[rh * DH + lane + 64 * k] = (half_t)(den > 0.f ? num[k] / den : 0.f);
+}
+
+struct Plan {
+  int nt, chunks, wpu, splits;
+  int64_t units;
+};
+size_t part_bytes(int64_t rows_heads, int splits, int dh) { return splits > 1 ? align_up((size_t)rows_heads * splits * (dh + 2) * 4, 256) : 0; }
+
+Plan plan_i8(int32_t nh, int32_t nkv, int32_t beams, int32_t b, int32_t table_stride) {
+  Plan p;
+  const int nq = nh / nkv * beams;
+  p.nt = nq <= 4 ? 1 : (nq <= 8 ? 2 : 4);
+  p.chunks = (int)ceil_div(nq, 4 * p.nt);
+  p.units = (int64_t)(b / beams) * nkv * p.chunks;
+  p.wpu = p.units >= 2048 ? 1 : (p.units >= 1024 ? 2 : 4);
+  const int64_t want = ceil_div(1024, p.units), most = ceil_div(table_stride, 8);   // two pages a wave at least
+  p.splits = p.wpu < 4 ? 1 : (int)(want < most ? want : most);
+  if (p.splits > 128) p.splits = 128;
+  if (p.splits < 1) p.splits = 1;
+  return p;
 }
 
 }  // namespace
 
-size_t decode_attention_i8_workspace(int32_t nkv, int32_t beams, int32_t b, int32_t dh, int32_t table_stride) {
-  (void)nkv, (void)beams, (void)b, (void)dh, (void)table_stride;
-  return 256;
+size_t decode_attention_i8_workspace(int32_t nh, int32_t nkv, int32_t beams, int32_t b, int32_t dh, int32_t table_stride) {
+  const Plan p = plan_i8(nh, nkv, beams, b, table_stride);
+  return part_bytes((int64_t)b * nh, p.splits, dh) + 256;
 }
 
 int decode_attention_i8_launch(const fg_model_cfg& cfg, int32_t nkv, int32_t beams, const half_t* q, int64_t q_stride, int32_t b,
                                const fg_kv_pages& pages, const fg_ragged& seqs, int32_t rows_bias, half_t* out, void* ws,
                                size_t ws_bytes, hipStream_t stream) {
-  (void)beams, (void)ws, (void)ws_bytes;
   if (b == 0) return FG_OK;
-  AttnI8Args a;
   const int dh = cfg.h1 / cfg.nh;
+  Plan p = plan_i8(cfg.nh, nkv, beams, b, seqs.table_stride);
+  const int64_t rh = (int64_t)b * cfg.nh;
+  if (rh > 0x7fffffff) return FG_ERR_SHAPE;
+  while (p.splits > 1 && (!ws || ws_bytes < part_bytes(rh, p.splits, dh))) p.splits = ws ? p.splits - 1 : 1;
+  AttnI8Args a;
   a.q = q;
   a.q_stride = q_stride;
   a.k_codes = reinterpret_cast<const int8_t*>(pages.k_codes);
@@ -89,22 +429,49 @@ int decode_attention_i8_launch(const fg_model_cfg& cfg, int32_t nkv, int32_t bea
   a.page_table = seqs.page_table;
   a.seq_ids = seqs.seq_ids;
   a.seq_rows = seqs.pos;
-  a.b = b;
   a.nh = cfg.nh;
   a.nkv = nkv;
+  a.beams = beams;
+  a.n_units = (int)p.units;
+  a.chunks = p.chunks;
   a.table_stride = seqs.table_stride;
   a.n_seqs = seqs.n_seqs;
   a.n_pages = pages.n_pages;
   a.rows_bias = rows_bias;
   a.scale = 1.0f / sqrtf((float)dh);
-  const int64_t waves = (int64_t)b * cfg.nh;
-  if (waves > 0x7fffffff) return FG_ERR_SHAPE;
+  a.splits = p.splits;
+  a.part_o = reinterpret_cast<float*>(ws);
+  a.part_ml = reinterpret_cast<float2*>(a.part_o + (p.splits > 1 ? rh * p.splits * dh : 0));
+  const dim3 grid((unsigned)ceil_div(p.units * p.wpu, 4), (unsigned)p.splits);
+  const size_t lds = beams > 1 ? (size_t)4 * 64 * beams * sizeof(uint2) : 0;
   ProfScope prof(FG_K_ATTN_DECODE, stream);
-  if (dh == 128)
-    hipLaunchKernelGGL(attn_decode_i8_kernel<128>, dim3((unsigned)waves), dim3(64), 0, stream, a);
-  else
-    hipLaunchKernelGGL(attn_decode_i8_kernel<64>, dim3((unsigned)waves), dim3(64), 0, stream, a);
+#define FG_I8(DH_, NT_, WPU_, SH_) hipLaunchKernelGGL((attn_decode_i8_kernel<DH_, NT_, WPU_, SH_>), grid, dim3(256), lds, stream, a)
+#define FG_I8_SH(DH_, NT_, WPU_)                                                     \
+  do {                                                                               \
+    if (beams > 1) FG_I8(DH_, NT_, WPU_, true); else FG_I8(DH_, NT_, WPU_, false);   \
+  } while (0)
+#define FG_I8_WPU(DH_, NT_)                                                                                       \
+  do {                                                                                                            \
+    if (p.wpu == 1) FG_I8_SH(DH_, NT_, 1); else if (p.wpu == 2) FG_I8_SH(DH_, NT_, 2); else FG_I8_SH(DH_, NT_, 4); \
+  } while (0)
+#define FG_I8_NT(DH_)                                                                                  \
+  do {                                                                                                 \
+    if (p.nt == 1) FG_I8_WPU(DH_, 1); else if (p.nt == 2) FG_I8_WPU(DH_, 2); else FG_I8_WPU(DH_, 4);   \
+  } while (0)
+  if (dh == 128) FG_I8_NT(128); else FG_I8_NT(64);
+#undef FG_I8_NT
+#undef FG_I8_WPU
+#undef FG_I8_SH
+#undef FG_I8
   FG_LAUNCH_CHECK();
+  if (p.splits > 1) {
+    const dim3 mg((unsigned)ceil_div(rh, 4));
+    if (dh == 128)
+      hipLaunchKernelGGL(attn_merge_i8_kernel<128>, mg, dim3(256), 0, stream, a, rh);
+    else
+      hipLaunchKernelGGL(attn_merge_i8_kernel<64>, mg, dim3(256), 0, stream, a, rh);
+    FG_LAUNCH_CHECK();
+  }
   return FG_OK;
 }
 
@@ -119,7 +486,7 @@ static bool beams_ok(const fg_model_cfg* cfg, int32_t nkv, int32_t beams, int32_
 extern "C" size_t fg_decode_attention_beams_workspace_bytes(const fg_model_cfg* cfg, int32_t nkv, int32_t beams, int32_t b,
                                                             int32_t table_stride) {
   if (!cfg || check_cfg(cfg) || !beams_ok(cfg, nkv, beams, b) || b == 0 || table_stride <= 0) return 0;
-  return decode_attention_i8_workspace(nkv, beams, b, cfg->h1 / cfg->nh, table_stride);
+  return decode_attention_i8_workspace(cfg->nh, nkv, beams, b, cfg->h1 / cfg->nh, table_stride);
 }
 
 extern "C" int fg_decode_attention_beams_paged(const fg_model_cfg* cfg, int32_t nkv, int32_t beams, const void* q_f16,
@@ -138,7 +505,7 @@ extern "C" int fg_decode_attention_beams_paged(const fg_model_cfg* cfg, int32_t 
   if (b == 0) return FG_OK;
   if (!q_f16 || !out_f16) return FG_ERR_NULL;
   if (((uintptr_t)q_f16 | (uintptr_t)out_f16) & 15u) return FG_ERR_SHAPE;
-  if (!ws || ws_bytes < decode_attention_i8_workspace(nkv, beams, b, cfg->h1 / cfg->nh, seqs->table_stride)) return FG_ERR_WORKSPACE;
+  if (!ws || ws_bytes < decode_attention_i8_workspace(cfg->nh, nkv, beams, b, cfg->h1 / cfg->nh, seqs->table_stride)) return FG_ERR_WORKSPACE;
   if ((uintptr_t)ws & 15u) return FG_ERR_SHAPE;
   return decode_attention_i8_launch(*cfg, nkv, beams, reinterpret_cast<const half_t*>(q_f16), q_row_stride, b, *pages, *seqs,
                                     rows_bias, reinterpret_cast<half_t*>(out_f16), ws, ws_bytes, as_stream(stream));

@@ -144,7 +144,7 @@ int check_pages(const fg_model_cfg* cfg, const fg_kv_pages* pages, const fg_ragg
 // workspace, or with less than decode_attention_i8_workspace, sequences are split over fewer workgroups
 int kv_append_i8_launch(const fg_model_cfg& cfg, const half_t* k, const half_t* v, int64_t row_stride, int32_t b, int32_t s,
                         const fg_kv_pages& pages, const fg_ragged& seqs, bool use_pos, hipStream_t stream);
-size_t decode_attention_i8_workspace(int32_t nkv, int32_t beams, int32_t b, int32_t dh, int32_t table_stride);
+size_t decode_attention_i8_workspace(int32_t nh, int32_t nkv, int32_t beams, int32_t b, int32_t dh, int32_t table_stride);
 int decode_attention_i8_launch(const fg_model_cfg& cfg, int32_t nkv, int32_t beams, const half_t* q, int64_t q_stride, int32_t b,
                                const fg_kv_pages& pages, const fg_ragged& seqs, int32_t rows_bias, half_t* out, void* ws,
                                size_t ws_bytes, hipStream_t stream);
