@@ -405,7 +405,7 @@ int64_t fg_diagonal_pages_needed(int32_t n_seqs, int32_t s, int32_t n, int32_t g
 /* ---- Beam search ---------------------------------------------------------------------------
  * n_groups sequences with `beams` rows each (1 <= beams <= FG_MAX_BEAMS); row g*beams + j is beam j of sequence g.
  *
- * fg_beam_select: of all continuations (beam j, word w) of a sequence, worth
+ * fg_beam_select (up to 65535 rows, vocab < 2^28): of all continuations (beam j, word w) of a sequence, worth
  *   v = scores[j] + logits[j][w] - log(sum over w' of exp(logits[j][w'])),
  * the n_best (1 .. FG_MAX_BEST) of the largest v, in descending order; among equal ones the larger logit, then the
  * lowest j * vocab + w comes first.  v is compared in binary64 and returned in binary32.

@@ -8,14 +8,120 @@ namespace fg {
 namespace {
 
 // ---------------------------------------------------------------- selection
-// A forbidden word is -inf (also NaN); +inf counts as the largest finite number.
-__device__ __forceinline__ float clean(float x) { return x > FLT_MAX ? FLT_MAX : (x >= -FLT_MAX ? x : -INFINITY); }
+// Two launches.  The first reads every logit once: a workgroup takes one piece of one row into registers and leaves the piece's
+// maximum, its sum of exponentials and its n_best words.  The second takes a sequence: what all pieces of all its beams left.
+//
+// The n best of a workgroup's values without sorting them: of the largest values of the 64 groups of four threads, the n-th
+// largest is a bound that at least n values reach, and (values falling as they may) few more.  Those are collected in LDS and
+// each counts how many are better: its place.  Should more than kList reach the bound (equal values, mostly), the best are
+// taken one after the other instead.  Values carry their place in the key, so no two are equal.
+//
+// The sum of exponentials decides between words of different beams and so is kept better than one binary32 exponential is:
+// exp(y) = 2^h (1 + ln 2 l), y = x - max, with h + l = y log2 e to twice the precision; added up in binary32 over a thread's 8 or
+// 32 values and in binary64 from there on.  What is left are the roundings of y (none for words within a factor of two of the
+// largest) and of the exponential instruction itself, some 2^-24 of each word's share and of either sign.
+constexpr int kList = 512;
 
-// What a row leaves behind: the logarithm of its sum of exponentials and its best words, (logit, word) in descending order.
-struct Best {
-  float x;
-  int32_t w;
+// A forbidden word is -inf (also NaN); +inf counts as the largest finite number.
+__device__ __forceinline__ float clean(float x) { return x >= -FLT_MAX ? fminf(x, FLT_MAX) : -INFINITY; }
+
+// order-preserving bits: larger number, larger key
+__device__ __forceinline__ uint32_t ordered(float x) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, x);
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float from_ordered(uint32_t u) {
+  return __builtin_bit_cast(float, u & 0x80000000u ? u & 0x7fffffffu : ~u);
+}
+__device__ __forceinline__ uint64_t ordered(double x) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  return u >> 63 ? ~u : u | (1ull << 63);
+}
+
+// Keys: of a piece's words (logit, lower word first); of a sequence's continuations (value, logit, lower beam, lower word).
+// All zero: none.
+struct Key1 {
+  uint64_t k;
+  __device__ __forceinline__ bool operator<(const Key1& o) const { return k < o.k; }
+  __device__ __forceinline__ bool none() const { return k == 0; }
 };
+struct Key2 {
+  uint64_t v, k;
+  __device__ __forceinline__ bool operator<(const Key2& o) const { return v < o.v || (v == o.v && k < o.k); }
+  __device__ __forceinline__ bool none() const { return v == 0; }
+};
+template <int CTRL>
+__device__ __forceinline__ uint64_t dpp64(uint64_t v) {
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, true);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(v >> 32), CTRL, 0xF, 0xF, true);
+  return (uint64_t)hi << 32 | lo;
+}
+template <int CTRL>
+__device__ __forceinline__ Key1 dpp(Key1 a) { return {dpp64<CTRL>(a.k)}; }
+template <int CTRL>
+__device__ __forceinline__ Key2 dpp(Key2 a) { return {dpp64<CTRL>(a.v), dpp64<CTRL>(a.k)}; }
+template <class K>
+__device__ __forceinline__ K larger(K a, K b) { return a < b ? b : a; }
+
+// The n (<= 32) largest keys of a workgroup of 256 threads.  mine: the largest of the thread's, or a lower bound of it that one
+// of its keys reaches.  each(bound, f) calls f for every key of the thread that reaches the bound (and may for others, none()
+// included).  emit(place, key) is called once for every place below the number found, which is returned.
+template <class K, class Each, class Emit>
+__device__ __forceinline__ int block_best(int n, K mine, K* list /* [kList] */, K* tops /* [64] */, K* bound_at, int* count, Each each,
+                                          Emit emit) {
+  const int tid = threadIdx.x;
+  K top = larger(mine, dpp<kDppXor1>(mine));
+  top = larger(top, dpp<kDppXor2>(top));
+  if ((tid & 3) == 0) tops[tid >> 2] = top;
+  if (tid == 0) *count = 0, *bound_at = {};
+  __syncthreads();
+  if (tid < 64) {
+    const K me = tops[tid];
+    int above = 0;
+    for (int i = 0; i < 64; ++i) above += me < tops[i] || (i < tid && !(tops[i] < me)) ? 1 : 0;   // lower bounds may be equal
+    if (above == n - 1) *bound_at = me;
+  }
+  __syncthreads();
+  const K bound = *bound_at;
+  each(bound, [&](K k) {
+    if (k.none() || k < bound) return;
+    const int at = atomicAdd(count, 1);
+    if (at < kList) list[at] = k;
+  });
+  __syncthreads();
+  const int found = *count;
+  if (found <= kList) {
+    for (int c = tid; c < found; c += 256) {
+      const K k = list[c];
+      int place = 0;
+      for (int i = 0; i < found; ++i) place += k < list[i] ? 1 : 0;
+      if (place < n) emit(place, k);
+    }
+    return found < n ? found : n;
+  }
+  K last = {};
+  for (int p = 0; p < n; ++p) {   // more than n reach the bound: there is always a next one
+    K best = {};
+    each(bound, [&](K k) {
+      if (!k.none() && (p == 0 || k < last) && best < k) best = k;
+    });
+    best = larger(best, dpp<kDppXor1>(best));
+    best = larger(best, dpp<kDppXor2>(best));
+    if ((tid & 3) == 0) tops[tid >> 2] = best;
+    __syncthreads();
+    last = tops[tid & 63];
+    __syncthreads();   // read before the next round writes
+    for (int m = 1; m < 64; m <<= 1) {
+      K o = last;
+      uint32_t* w = reinterpret_cast<uint32_t*>(&o);
+#pragma unroll
+      for (int i = 0; i < (int)(sizeof(K) / 4); ++i) w[i] = (uint32_t)__shfl_xor((int)w[i], m, 64);
+      last = larger(last, o);
+    }
+    if (tid == 0) emit(p, last);
+  }
+  return n;
+}
 
 struct SelectArgs {
   const float* logits;
@@ -23,94 +129,179 @@ struct SelectArgs {
   const float* scores;
   const int32_t* done;
   int32_t eos, vocab, beams, n_best;
-  double* lse;    // [rows]
-  Best* best;     // [rows][n_best], word -1: none
+  int32_t pieces, piece;   // of a row, and words of one
+  double* sums;            // [rows][pieces]: sum of exp(x - ref); 0: no words
+  double* refs;            // [rows][pieces]
+  uint64_t* best;          // [rows][pieces][n_best] keys, 0: none
   int32_t* out_beams;
   int32_t* out_ids;
   float* out_scores;
   int32_t* out_done;
 };
 
-// One workgroup per row; the best words one after the other, each the largest below the one before.
+constexpr uint32_t kMostWord = (1u << 28) - 1;
+
+template <int VPT, bool VEC>
 __global__ __launch_bounds__(256) void beam_rows_kernel(SelectArgs a) {
-  __shared__ float sx[256];
-  __shared__ int sw[256];
-  __shared__ double ss[256];
-  const int row = blockIdx.x, tid = threadIdx.x;
-  const float* x = a.logits + (int64_t)row * a.ld;
-  float px = INFINITY;   // the word chosen last
-  int pw = -1;
-  float top = 0.f;
-  for (int n = 0; n < a.n_best; ++n) {
-    float bx = -INFINITY;
-    int bw = -1;
-    for (int w = tid; w < a.vocab; w += 256) {
-      const float v = clean(x[w]);
-      if (v == -INFINITY || v > px || (v == px && w <= pw)) continue;
-      if (v > bx) bx = v, bw = w;
+  __shared__ Key1 list[kList], tops[64], bound;
+  __shared__ double part[4];
+  __shared__ float wave_top[4];
+  __shared__ int count;
+  const int row = blockIdx.y, tid = threadIdx.x;
+  if (a.done && a.done[row]) return;   // nobody reads what it would leave
+  const int w0 = blockIdx.x * a.piece, n = min(a.piece, a.vocab - w0);   // words of this piece (a multiple of 4 if VEC)
+  const float* src = a.logits + (int64_t)row * a.ld + w0;
+  float x[VPT];
+  auto word = [&](int j) { return VEC ? (j >> 2) * 1024 + tid * 4 + (j & 3) : j * 256 + tid; };
+  if constexpr (VEC) {
+#pragma unroll
+    for (int j = 0; j < VPT; j += 4) {
+      const int w = word(j);
+      float4 v = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+      if (w < n) v = *reinterpret_cast<const float4*>(src + w);
+      x[j] = v.x, x[j + 1] = v.y, x[j + 2] = v.z, x[j + 3] = v.w;
     }
-    sx[tid] = bx, sw[tid] = bw;
-    __syncthreads();
-    for (int o = 128; o > 0; o >>= 1) {
-      if (tid < o && sw[tid + o] >= 0 && (sw[tid] < 0 || sx[tid + o] > sx[tid] || (sx[tid + o] == sx[tid] && sw[tid + o] < sw[tid])))
-        sx[tid] = sx[tid + o], sw[tid] = sw[tid + o];
-      __syncthreads();
-    }
-    px = sx[0], pw = sw[0];
-    if (n == 0) top = px;
-    if (tid == 0) a.best[(int64_t)row * a.n_best + n] = {px, pw};
-    __syncthreads();
-    if (pw < 0) {
-      for (int k = n + 1 + tid; k < a.n_best; k += 256) a.best[(int64_t)row * a.n_best + k] = {-INFINITY, -1};
-      break;
+  } else {
+#pragma unroll
+    for (int j = 0; j < VPT; ++j) {
+      const int w = word(j);
+      x[j] = w < n ? src[w] : -INFINITY;
     }
   }
-  double s = 0.0;
-  if (top > -INFINITY)
-    for (int w = tid; w < a.vocab; w += 256) s += exp((double)clean(x[w]) - (double)top);
-  ss[tid] = s;
+  float top = -INFINITY;
+#pragma unroll
+  for (int j = 0; j < VPT; ++j) {
+    x[j] = clean(x[j]);
+    top = fmaxf(top, x[j]);
+  }
+  const float wt = wave_max(top);
+  if ((tid & 63) == 0) wave_top[tid >> 6] = wt;
   __syncthreads();
-  for (int o = 128; o > 0; o >>= 1) {
-    if (tid < o) ss[tid] += ss[tid + o];
-    __syncthreads();
+  const float m = fmaxf(fmaxf(wave_top[0], wave_top[1]), fmaxf(wave_top[2], wave_top[3]));
+  const int64_t rp = (int64_t)row * a.pieces + blockIdx.x;
+  constexpr float L = 1.44269502f, Ll = 1.92596299e-8f;   // log2 e in two binary32 numbers
+  float s = 0.f;
+#pragma unroll
+  for (int j = 0; j < VPT; ++j) {
+    const float y = fmaxf(x[j] - m, -150.f);   // 2^-216 is 0; a piece without words (-inf - -inf) comes here too
+    const float h = y * L, l = __builtin_fmaf(y, Ll, __builtin_fmaf(y, L, -h));
+    const float e = __builtin_amdgcn_exp2f(h);
+    s += __builtin_fmaf(e, l * 0.693147181f, e);
   }
-  if (tid == 0) a.lse[row] = top > -INFINITY ? (double)top + log(ss[0]) : 0.0;
+  double d = (double)s;
+  for (int k = 1; k < 64; k <<= 1) d += __shfl_xor(d, k, 64);
+  if ((tid & 63) == 0) part[tid >> 6] = d;
+  auto key = [&](int j) -> Key1 {
+    const uint64_t k = (uint64_t)ordered(x[j]) << 32 | (uint32_t)(kMostWord - (uint32_t)(w0 + word(j)));
+    return {x[j] > -INFINITY ? k : 0};
+  };
+  const Key1 mine = {top > -INFINITY ? (uint64_t)ordered(top) << 32 : 0};
+  const int found = block_best<Key1>(
+      a.n_best, mine, list, tops, &bound, &count,
+      [&](Key1 least, auto f) {
+        const float lx = least.none() ? -INFINITY : from_ordered((uint32_t)(least.k >> 32));
+#pragma unroll
+        for (int j = 0; j < VPT; ++j)
+          if (x[j] >= lx) f(key(j));
+      },
+      [&](int place, Key1 k) { a.best[rp * a.n_best + place] = k.k; });
+  if (tid >= found && tid < a.n_best) a.best[rp * a.n_best + tid] = 0;
+  if (tid == 0) {   // (the waves' sums were written before the barriers above)
+    a.sums[rp] = part[0] + part[1] + part[2] + part[3];
+    a.refs[rp] = m;
+  }
 }
 
-// One thread per sequence.
-__global__ __launch_bounds__(64) void beam_merge_kernel(SelectArgs a, int n_groups) {
-  const int g = blockIdx.x * 64 + threadIdx.x;
-  if (g >= n_groups) return;
-  int at[FG_MAX_BEAMS] = {};   // the next of every beam's list
-  for (int n = 0; n < a.n_best; ++n) {
-    double bv = -INFINITY;
-    float bx = 0.f;
-    int bj = -1, bw = -1;
-    for (int j = 0; j < a.beams; ++j) {
-      const int64_t row = (int64_t)g * a.beams + j;
-      const float sc = a.scores[row];
-      if (!(sc > -INFINITY) || at[j] >= a.n_best) continue;
-      double v;
-      float x = 0.f;
-      int w;
-      if (a.done && a.done[row]) {
-        if (at[j] > 0) continue;
-        v = sc, w = a.eos;
-      } else {
-        const Best b = a.best[row * a.n_best + at[j]];
-        if (b.w < 0) continue;
-        v = (double)sc + ((double)b.x - a.lse[row]), x = b.x, w = b.w;
-      }
-      if (bj < 0 || v > bv || (v == bv && x > bx)) bv = v, bx = x, bj = j, bw = w;   // beams in order: the lowest wins ties
-    }
-    const int64_t o = (int64_t)g * a.n_best + n;
-    if (bj >= 0) ++at[bj];
-    a.out_beams[o] = bj;
-    a.out_ids[o] = bw;
-    a.out_scores[o] = bj < 0 ? -INFINITY : (float)bv;
-    if (a.out_done)
-      a.out_done[o] = bj < 0 || (a.done && a.done[(int64_t)g * a.beams + bj]) || (a.eos >= 0 && bw == a.eos) ? 1 : 0;
+// One workgroup per sequence.  HELD: the keys of its continuations fit into LDS (kHeld) and are made once.
+constexpr int kHeld = 2048;
+template <bool HELD>
+__global__ __launch_bounds__(256) void beam_merge_kernel(SelectArgs a) {
+  __shared__ Key2 list[kList], tops[64], bound;
+  __shared__ Key2 held[HELD ? kHeld : 1];
+  __shared__ double lse[FG_MAX_BEAMS], score[FG_MAX_BEAMS];
+  __shared__ int state[FG_MAX_BEAMS];   // 0: out, 1: alive, 2: done
+  __shared__ int count;
+  const int g = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+  const int64_t row0 = (int64_t)g * a.beams;
+  const int per_beam = a.pieces * a.n_best, total = a.beams * per_beam;
+  const uint64_t* best = a.best + row0 * per_beam;
+  // the words are on their way while the sums are put together
+  uint64_t raw[HELD ? kHeld / 256 : 1];
+  if constexpr (HELD) {
+#pragma unroll
+    for (int i = 0; i < kHeld / 256; ++i) raw[i] = tid + 256 * i < total ? best[tid + 256 * i] : 0;
   }
+  for (int j = tid >> 6; j < a.beams; j += 4) {   // a wave per beam
+    const bool over = a.done && a.done[row0 + j];
+    const float sc = a.scores[row0 + j];
+    const int64_t rp = (row0 + j) * a.pieces;
+    double ref = -INFINITY, s = 0.0;
+    if (!over) {
+      for (int p0 = 0; p0 < a.pieces; p0 += 64) {
+        const int p = p0 + lane;
+        const double sp = p < a.pieces ? a.sums[rp + p] : 0.0, rf = p < a.pieces ? a.refs[rp + p] : 0.0;
+        double top = sp > 0.0 ? rf : -INFINITY;
+        for (int k = 1; k < 64; k <<= 1) top = fmax(top, __shfl_xor(top, k, 64));
+        const double now = fmax(ref, top);
+        s = ref > -INFINITY ? s * exp(ref - now) : 0.0;   // (one round unless there are over 64 pieces)
+        double t = sp > 0.0 ? sp * exp(rf - now) : 0.0;
+        for (int k = 1; k < 64; k <<= 1) t += __shfl_xor(t, k, 64);
+        s += t;
+        ref = now;
+      }
+    }
+    if (lane == 0) {
+      lse[j] = s > 0.0 ? ref + log(s) : 0.0;
+      score[j] = sc;
+      state[j] = !(sc > -INFINITY) ? 0 : (over ? 2 : 1);
+    }
+  }
+  __syncthreads();
+  auto key = [&](int t, uint64_t b) -> Key2 {
+    const int j = t / per_beam;
+    if (state[j] == 2)   // finished: its first place is the one it has to offer
+      return t == j * per_beam
+                 ? Key2{ordered(score[j]), (uint64_t)ordered(0.f) << 32 | (uint64_t)(FG_MAX_BEAMS - 1 - j) << 28 | (kMostWord - (uint32_t)a.eos)}
+                 : Key2{0, 0};
+    if (state[j] == 0 || b == 0) return {0, 0};
+    const double v = score[j] + ((double)from_ordered((uint32_t)(b >> 32)) - lse[j]);
+    return {ordered(v), (b & 0xffffffff0fffffffull) | (uint64_t)(FG_MAX_BEAMS - 1 - j) << 28};
+  };
+  Key2 mine = {0, 0};
+  if constexpr (HELD) {
+#pragma unroll
+    for (int i = 0; i < kHeld / 256; ++i)
+      if (tid + 256 * i < total) {
+        const Key2 k = key(tid + 256 * i, raw[i]);
+        held[tid + 256 * i] = k;   // read by this thread only
+        mine = larger(mine, k);
+      }
+  } else {
+    for (int t = tid; t < total; t += 256) mine = larger(mine, key(t, best[t]));
+  }
+  const int64_t o0 = (int64_t)g * a.n_best;
+  auto put = [&](int place, int j, int w, float v, int done) {
+    a.out_beams[o0 + place] = j;
+    a.out_ids[o0 + place] = w;
+    a.out_scores[o0 + place] = v;
+    if (a.out_done) a.out_done[o0 + place] = done;
+  };
+  const int found = block_best<Key2>(
+      a.n_best, mine, list, tops, &bound, &count,
+      [&](Key2, auto f) {
+        for (int t = tid; t < total; t += 256) {
+          if constexpr (HELD)
+            f(held[t]);
+          else
+            f(key(t, best[t]));
+        }
+      },
+      [&](int place, Key2 k) {
+        const int j = FG_MAX_BEAMS - 1 - (int)(k.k >> 28 & 15), w = (int)(kMostWord - (uint32_t)(k.k & kMostWord));
+        const uint64_t u = k.v >> 63 ? k.v & ~(1ull << 63) : ~k.v;
+        put(place, j, w, (float)__builtin_bit_cast(double, u), state[j] == 2 || (a.eos >= 0 && w == a.eos) ? 1 : 0);
+      });
+  if (tid >= found && tid < a.n_best) put(tid, -1, -1, -INFINITY, 1);
 }
 
 // ---------------------------------------------------------------- reordering
@@ -223,18 +414,38 @@ __global__ __launch_bounds__(256) void beam_copy_kernel(CopyArgs a) {
   }
 }
 
+// Words of a row that a workgroup takes: 8192 where the rows alone fill the chip, else 2048.  512 rows of 50272: see below
+struct SelectPlan {
+  int vpt, pieces, piece;
+};
+SelectPlan plan_select(int64_t rows, int vocab) {
+  SelectPlan p;
+  p.vpt = rows * ceil_div(vocab, 8192) >= 512 ? 32 : 8;
+  p.pieces = (int)ceil_div(vocab, 256 * p.vpt);
+  p.piece = (int)align_up((size_t)ceil_div(vocab, p.pieces), 4);   // even: every group of threads has words
+  p.pieces = (int)ceil_div(vocab, p.piece);
+  return p;
+}
+
 struct SelectWs {
-  double* lse;
-  Best* best;
+  double* sums;
+  double* refs;
+  uint64_t* best;
   size_t total;
 };
-SelectWs carve_select_ws(int64_t rows, int n_best, void* base) {
+SelectWs carve_select_ws(int64_t rows, const SelectPlan& p, int n_best, void* base) {
   SelectWs W;
-  unsigned char* p = reinterpret_cast<unsigned char*>(base);
-  const size_t lse = align_up((size_t)rows * 8, 256);
-  W.lse = reinterpret_cast<double*>(p);
-  W.best = reinterpret_cast<Best*>(p ? p + lse : nullptr);
-  W.total = lse + align_up((size_t)rows * n_best * sizeof(Best), 256);
+  unsigned char* b = reinterpret_cast<unsigned char*>(base);
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    unsigned char* r = b ? b + off : nullptr;
+    off += align_up(bytes, 256);
+    return r;
+  };
+  W.sums = reinterpret_cast<double*>(take((size_t)rows * p.pieces * 8));
+  W.refs = reinterpret_cast<double*>(take((size_t)rows * p.pieces * 8));
+  W.best = reinterpret_cast<uint64_t*>(take((size_t)rows * p.pieces * n_best * 8));
+  W.total = off;
   return W;
 }
 
@@ -252,7 +463,9 @@ using namespace fg;
 
 extern "C" size_t fg_beam_select_workspace_bytes(const fg_model_cfg* cfg, int32_t n_groups, int32_t beams, int32_t n_best) {
   if (!cfg || check_cfg(cfg) || !groups_ok(n_groups, beams) || n_groups == 0 || n_best < 1 || n_best > FG_MAX_BEST) return 0;
-  return carve_select_ws((int64_t)n_groups * beams, n_best, nullptr).total;
+  if (cfg->vocab > (int)kMostWord || (int64_t)n_groups * beams > 65535) return 0;
+  const int64_t rows = (int64_t)n_groups * beams;
+  return carve_select_ws(rows, plan_select(rows, cfg->vocab), n_best, nullptr).total;
 }
 
 extern "C" int fg_beam_select(const fg_model_cfg* cfg, int32_t n_groups, int32_t beams, int32_t n_best, const float* logits,
@@ -262,20 +475,37 @@ extern "C" int fg_beam_select(const fg_model_cfg* cfg, int32_t n_groups, int32_t
   const int rc = check_cfg(cfg);
   if (rc) return rc;
   if (!groups_ok(n_groups, beams) || n_best < 1 || n_best > FG_MAX_BEST || row_stride < cfg->vocab) return FG_ERR_SHAPE;
-  if (eos >= cfg->vocab || (done && eos < 0)) return FG_ERR_SHAPE;
+  if (eos >= cfg->vocab || (done && eos < 0) || cfg->vocab > (int)kMostWord) return FG_ERR_SHAPE;
+  if ((int64_t)n_groups * beams > 65535) return FG_ERR_SHAPE;
   if (n_groups == 0) return FG_OK;
   if (!logits || !scores || !out_beams || !out_ids || !out_scores) return FG_ERR_NULL;
   const int64_t rows = (int64_t)n_groups * beams;
-  const SelectWs W = carve_select_ws(rows, n_best, ws);
+  const SelectPlan p = plan_select(rows, cfg->vocab);
+  const SelectWs W = carve_select_ws(rows, p, n_best, ws);
   if (!ws || ws_bytes < W.total) return FG_ERR_WORKSPACE;
   if ((uintptr_t)ws & 15u) return FG_ERR_SHAPE;
-  const SelectArgs a = {logits, row_stride, scores, done, eos, cfg->vocab, beams, n_best, W.lse, W.best, out_beams, out_ids,
-                        out_scores, out_done};
+  const SelectArgs a = {logits, row_stride, scores, done, eos, cfg->vocab, beams, n_best, p.pieces, p.piece, W.sums, W.refs, W.best,
+                        out_beams, out_ids, out_scores, out_done};
+  const bool vec = ((uintptr_t)logits & 15u) == 0 && row_stride % 4 == 0 && cfg->vocab % 4 == 0;
+  const dim3 grid((unsigned)p.pieces, (unsigned)rows);
   hipStream_t st = as_stream(stream);
   ProfScope prof(FG_K_BEAM_SELECT, st);
-  hipLaunchKernelGGL(beam_rows_kernel, dim3((unsigned)rows), dim3(256), 0, st, a);
+  if (p.vpt == 32) {
+    if (vec)
+      hipLaunchKernelGGL((beam_rows_kernel<32, true>), grid, dim3(256), 0, st, a);
+    else
+      hipLaunchKernelGGL((beam_rows_kernel<32, false>), grid, dim3(256), 0, st, a);
+  } else {
+    if (vec)
+      hipLaunchKernelGGL((beam_rows_kernel<8, true>), grid, dim3(256), 0, st, a);
+    else
+      hipLaunchKernelGGL((beam_rows_kernel<8, false>), grid, dim3(256), 0, st, a);
+  }
   FG_LAUNCH_CHECK();
-  hipLaunchKernelGGL(beam_merge_kernel, dim3((unsigned)ceil_div(n_groups, 64)), dim3(64), 0, st, a, n_groups);
+  if ((int64_t)beams * p.pieces * n_best <= kHeld)
+    hipLaunchKernelGGL(beam_merge_kernel<true>, dim3((unsigned)n_groups), dim3(256), 0, st, a);
+  else
+    hipLaunchKernelGGL(beam_merge_kernel<false>, dim3((unsigned)n_groups), dim3(256), 0, st, a);
   FG_LAUNCH_CHECK();
   return FG_OK;
 }
