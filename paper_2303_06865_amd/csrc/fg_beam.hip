@@ -1,6 +1,8 @@
 // Beam search: selection over the beams of a sequence and the vocabulary, and the page tables behind the beams chosen.
 #include <float.h>
 
+#include <type_traits>
+
 #include "fg_common.h"
 
 namespace fg {
@@ -60,6 +62,35 @@ template <int CTRL>
 __device__ __forceinline__ Key1 dpp(Key1 a) { return {dpp64<CTRL>(a.k)}; }
 template <int CTRL>
 __device__ __forceinline__ Key2 dpp(Key2 a) { return {dpp64<CTRL>(a.v), dpp64<CTRL>(a.k)}; }
+// over the wave, in registers: inside 16 lanes by DPP, then across
+template <class Op>
+__device__ __forceinline__ double wave_f64(double v, Op op) {
+  auto in16 = [&](auto ctrl) {
+    constexpr int c = decltype(ctrl)::value;
+    v = op(v, __builtin_bit_cast(double, dpp64<c>(__builtin_bit_cast(uint64_t, v))));
+  };
+  in16(std::integral_constant<int, kDppXor1>{});
+  in16(std::integral_constant<int, kDppXor2>{});
+  in16(std::integral_constant<int, kDppHalfMirror>{});
+  in16(std::integral_constant<int, kDppMirror>{});
+  auto pair = [&](const auto lo, const auto hi) {
+    v = op(__builtin_bit_cast(double, (uint64_t)(uint32_t)hi[0] << 32 | (uint32_t)lo[0]),
+           __builtin_bit_cast(double, (uint64_t)(uint32_t)hi[1] << 32 | (uint32_t)lo[1]));
+  };
+  uint64_t u = __builtin_bit_cast(uint64_t, v);
+  pair(__builtin_amdgcn_permlane16_swap((uint32_t)u, (uint32_t)u, false, false),
+       __builtin_amdgcn_permlane16_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false));
+  u = __builtin_bit_cast(uint64_t, v);
+  pair(__builtin_amdgcn_permlane32_swap((uint32_t)u, (uint32_t)u, false, false),
+       __builtin_amdgcn_permlane32_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false));
+  return v;
+}
+__device__ __forceinline__ double wave_sum_f64(double v) {
+  return wave_f64(v, [](double a, double b) { return a + b; });
+}
+__device__ __forceinline__ double wave_max_f64(double v) {
+  return wave_f64(v, [](double a, double b) { return fmax(a, b); });
+}
 template <class K>
 __device__ __forceinline__ K larger(K a, K b) { return a < b ? b : a; }
 
@@ -75,11 +106,15 @@ __device__ __forceinline__ int block_best(int n, K mine, K* list /* [kList] */, 
   if ((tid & 3) == 0) tops[tid >> 2] = top;
   if (tid == 0) *count = 0, *bound_at = {};
   __syncthreads();
-  if (tid < 64) {
-    const K me = tops[tid];
+  {   // four threads per group, a quarter of the others each
+    const int group = tid >> 2, from = (tid & 3) * 16;
+    const K me = tops[group];
     int above = 0;
-    for (int i = 0; i < 64; ++i) above += me < tops[i] || (i < tid && !(tops[i] < me)) ? 1 : 0;   // lower bounds may be equal
-    if (above == n - 1) *bound_at = me;
+#pragma unroll
+    for (int i = from; i < from + 16; ++i) above += me < tops[i] || (i < group && !(tops[i] < me)) ? 1 : 0;   // lower bounds may be equal
+    above += __builtin_amdgcn_update_dpp(0, above, kDppXor1, 0xF, 0xF, true);
+    above += __builtin_amdgcn_update_dpp(0, above, kDppXor2, 0xF, 0xF, true);
+    if ((tid & 3) == 0 && above == n - 1) *bound_at = me;
   }
   __syncthreads();
   const K bound = *bound_at;
@@ -188,8 +223,7 @@ __global__ __launch_bounds__(256) void beam_rows_kernel(SelectArgs a) {
     const float e = __builtin_amdgcn_exp2f(h);
     s += __builtin_fmaf(e, l * 0.693147181f, e);
   }
-  double d = (double)s;
-  for (int k = 1; k < 64; k <<= 1) d += __shfl_xor(d, k, 64);
+  const double d = wave_sum_f64((double)s);
   if ((tid & 63) == 0) part[tid >> 6] = d;
   auto key = [&](int j) -> Key1 {
     const uint64_t k = (uint64_t)ordered(x[j]) << 32 | (uint32_t)(kMostWord - (uint32_t)(w0 + word(j)));
@@ -240,13 +274,9 @@ __global__ __launch_bounds__(256) void beam_merge_kernel(SelectArgs a) {
       for (int p0 = 0; p0 < a.pieces; p0 += 64) {
         const int p = p0 + lane;
         const double sp = p < a.pieces ? a.sums[rp + p] : 0.0, rf = p < a.pieces ? a.refs[rp + p] : 0.0;
-        double top = sp > 0.0 ? rf : -INFINITY;
-        for (int k = 1; k < 64; k <<= 1) top = fmax(top, __shfl_xor(top, k, 64));
-        const double now = fmax(ref, top);
-        s = ref > -INFINITY ? s * exp(ref - now) : 0.0;   // (one round unless there are over 64 pieces)
-        double t = sp > 0.0 ? sp * exp(rf - now) : 0.0;
-        for (int k = 1; k < 64; k <<= 1) t += __shfl_xor(t, k, 64);
-        s += t;
+        const double now = fmax(ref, wave_max_f64(sp > 0.0 ? rf : -INFINITY));
+        if (p0 > 0 && ref > -INFINITY) s *= exp(ref - now);   // over 64 pieces
+        s += wave_sum_f64(sp > 0.0 ? sp * exp(rf - now) : 0.0);
         ref = now;
       }
     }
