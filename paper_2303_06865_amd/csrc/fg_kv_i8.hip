@@ -5,6 +5,8 @@
 // wider step: rint(c * (S / S')).  That happens about ln(64) times in a page's life when rows come one at a time, and not at
 // all when a page is filled by one call.  Every step of the arithmetic is one rounded binary32 operation (this file is
 // compiled without contraction and with IEEE division), so codes and scales are a function of the call sequence alone.
+#include <type_traits>
+
 #include "fg_common.h"
 
 namespace fg {
@@ -32,18 +34,49 @@ struct AppendI8Args {
   int8_t* codes[2];
   float* scales[2];
   int64_t ld;
-  int32_t b, s, nh, slots;   // slots: pages that the s rows of a sequence can touch
+  int32_t b, s, nh, slots, head_groups;   // slots: pages that the s rows of a sequence can touch; head_groups: workgroups a row of heads takes
   PageRows at;
 };
 
+// Codes of a page's new rows, and what becomes of the old ones.
+struct Step {
+  float old, now, ratio, inv;
+  bool grown;
+};
+__device__ __forceinline__ Step step_of(float top, float old, bool begun) {
+  Step s;
+  s.old = begun ? old : 0.f;
+  s.now = fmaxf(s.old, top / 127.0f);
+  s.grown = begun && s.now > s.old;
+  s.ratio = s.grown ? s.old / s.now : 1.f;
+  s.inv = s.now > 0.f ? 1.0f / s.now : 0.f;
+  return s;
+}
+__device__ __forceinline__ int8_t code_of(half_t v, const Step& s) { return (int8_t)(int)rintf((float)v * s.inv); }
+__device__ __forceinline__ int8_t again(int8_t c, const Step& s) { return (int8_t)(int)rintf((float)c * s.ratio); }
+__device__ __forceinline__ float abs_max(const h8_t v, float top) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf((float)v[e]));
+  return top;
+}
+
+// The units of 16 positions of a page's value codes in LDS, [group of 16][dh] in an order in which the lanes that hold eight
+// neighbouring dimensions each, as well as lanes that take units in order, meet few others on a bank.
+template <int DH>
+__device__ __forceinline__ int unit_at(int group, int d) {
+  return (group * DH + (d & ~7) + (((d & 7) + (d >> 3)) & 7)) * 16;
+}
+
 // One wave per (sequence of the call, page it touches, head, K or V).  Lane = 8 head dimensions (lane % LR) of NR
 // consecutive positions (lane / LR): a row of a head is read by LR lanes, 16 bytes each, and at head size 128 the
-// lane's 16 positions are one unit of the value codes' order.
+// lane's 16 positions are one unit of the value codes' order.  Values go through LDS, so that their units leave in order (straight
+// from the lanes, 16 bytes in every 128, 16 x 500 rows of 32 heads took 70 us instead of ~).
 template <int DH, bool VALUES>
-__device__ __forceinline__ void store_rows(const AppendI8Args& a, const half_t* src, int64_t ld, int8_t* codes, float* scale,
-                                           int lo, int hi, int lane) {
+__device__ __forceinline__ void store_rows(const half_t* src, int64_t ld, int8_t* codes, float* scale, int lo, int hi, int lane,
+                                           uint8_t* sm) {
   constexpr int LR = DH / 8, NR = LR;   // 64 positions over 64 / LR groups of lanes
   const int d0 = (lane % LR) * 8, r0 = (lane / LR) * NR;
+  const float was = lo > 0 ? *scale : 0.f;
   h8_t x[NR];
 #pragma unroll
   for (int n = 0; n < NR; ++n) {
@@ -52,67 +85,70 @@ __device__ __forceinline__ void store_rows(const AppendI8Args& a, const half_t* 
   }
   float top = 0.f;
 #pragma unroll
-  for (int n = 0; n < NR; ++n)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf((float)x[n][e]));
-  top = wave_max(top) / 127.0f;
-  const float old = lo > 0 ? *scale : 0.f;
-  const float now = fmaxf(old, top);
-  const bool grown = lo > 0 && now > old;   // the same in all lanes
-  const float ratio = grown ? old / now : 1.f;
-  const float inv = now > 0.f ? 1.0f / now : 0.f;
-  auto code = [&](half_t v) -> int8_t { return (int8_t)(int)rintf((float)v * inv); };
-  auto again = [&](int8_t c) -> int8_t { return (int8_t)(int)rintf((float)c * ratio); };
+  for (int n = 0; n < NR; ++n) top = abs_max(x[n], top);
+  const Step st = step_of(wave_max(top), was, lo > 0);   // the same in all lanes
   if constexpr (!VALUES) {
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
       const int r = r0 + n;
       i8x8_t* dst = reinterpret_cast<i8x8_t*>(codes + r * DH + d0);
       const bool fresh = r >= lo && r < hi;
-      if (fresh || grown) {
+      if (fresh || st.grown) {
         i8x8_t c;
         if (fresh) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) c[e] = code(x[n][e]);
+          for (int e = 0; e < 8; ++e) c[e] = code_of(x[n][e], st);
         } else {
-          const i8x8_t was = *dst;
+          const i8x8_t old = *dst;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) c[e] = again(was[e]);
+          for (int e = 0; e < 8; ++e) c[e] = again(old[e], st);
         }
         *dst = c;
       }
     }
   } else {
     const bool any = r0 < hi && r0 + NR > lo, all = r0 >= lo && r0 + NR <= hi;
-    if (any || grown) {
+    wave_lds_fence();   // what was read from there before has been
+    if (any || st.grown) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        // NR positions of dimension d0 + e: a unit of 16 bytes, or half of one at head size 64
-        i8x8_t* dst = reinterpret_cast<i8x8_t*>(codes + ((r0 >> 4) * DH + d0 + e) * 16 + (r0 & 15));
+      for (int e = 0; e < 8; ++e)
 #pragma unroll
         for (int n8 = 0; n8 < NR / 8; ++n8) {
+          const int r = r0 + 8 * n8;
           i8x8_t c = (i8x8_t)(int8_t)0;
-          if (!all) c = dst[n8];
+          if (!all) c = *reinterpret_cast<const i8x8_t*>(codes + ((r >> 4) * DH + d0 + e) * 16 + (r & 15));
 #pragma unroll
-          for (int n = 0; n < 8; ++n) {
-            const int r = r0 + 8 * n8 + n;
-            c[n] = r >= lo && r < hi ? code(x[8 * n8 + n][e]) : (grown ? again(c[n]) : c[n]);
-          }
-          dst[n8] = c;
+          for (int n = 0; n < 8; ++n)
+            c[n] = r + n >= lo && r + n < hi ? code_of(x[8 * n8 + n][e], st) : (st.grown ? again(c[n], st) : c[n]);
+          *reinterpret_cast<i8x8_t*>(sm + unit_at<DH>(r >> 4, d0 + e) + (r & 15)) = c;
         }
+    }
+    wave_lds_fence();
+#pragma unroll
+    for (int i = 0; i < DH / 16; ++i) {
+      const int u = 64 * i + lane, group = u / DH, d = u % DH;
+      // (at head size 64 a group of 16 positions is two lanes' work: a half that is not new is kept)
+      const bool lower = st.grown || (16 * group < hi && 16 * group + 8 > lo), upper = st.grown || (16 * group + 8 < hi && 16 * group + 16 > lo);
+      const uint8_t* from = sm + unit_at<DH>(group, d);
+      if (NR == 16 ? lower || upper : lower && upper) {
+        *reinterpret_cast<u4_t*>(codes + u * 16) = *reinterpret_cast<const u4_t*>(from);
+      } else if (NR == 8 && (lower || upper)) {
+        const int h = lower ? 0 : 8;
+        *reinterpret_cast<u2_t*>(codes + u * 16 + h) = *reinterpret_cast<const u2_t*>(from + h);
       }
     }
   }
-  if (lane == 0) *scale = now;
+  if (lane == 0) *scale = st.now;
 }
 
 template <int DH>
 __global__ __launch_bounds__(256) void kv_append_i8_kernel(AppendI8Args a) {
-  const int lane = threadIdx.x & 63;
-  const int head = blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  __shared__ __attribute__((aligned(16))) uint8_t sm[4][FG_PAGE_ROWS * DH];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int unit = blockIdx.x / a.head_groups, head = (blockIdx.x - unit * a.head_groups) * 4 + wave;
   if (head >= a.nh) return;
-  const int which = blockIdx.z;
-  const int i = blockIdx.x / a.slots, k = blockIdx.x - i * a.slots;
+  const int which = blockIdx.y;
+  const int i = unit / a.slots, k = unit - i * a.slots;
   const int sid = a.at.seq_ids ? a.at.seq_ids[i] : i;
   const int64_t p_i = a.at.pos ? a.at.pos[i] : 0;
   if (p_i < 0) return;
@@ -128,9 +164,9 @@ __global__ __launch_bounds__(256) void kv_append_i8_kernel(AppendI8Args a) {
     const int lo = (int)(first - s0), hi = (int)(p + a.s < s0 + 64 ? p + a.s - s0 : 64);
     const half_t* src = a.src[which] + ((int64_t)j * a.s + (first - p)) * a.ld + (int64_t)head * DH;
     if (which == 0)
-      store_rows<DH, false>(a, src, a.ld, codes, scale, lo, hi, lane);
+      store_rows<DH, false>(src, a.ld, codes, scale, lo, hi, lane, sm[wave]);
     else
-      store_rows<DH, true>(a, src, a.ld, codes, scale, lo, hi, lane);
+      store_rows<DH, true>(src, a.ld, codes, scale, lo, hi, lane, sm[wave]);
   };
   if (!a.at.seq_ids) {
     store(i, p_i);
@@ -152,6 +188,84 @@ __global__ __launch_bounds__(256) void kv_append_i8_kernel(AppendI8Args a) {
   }
 }
 
+// One new row per sequence (the decode step): DH / 8 lanes a head, eight or four heads a wave, K or V.  What is written are eight
+// bytes a lane, for V in eight units; only a page whose scale grows is read.
+template <int DH>
+__global__ __launch_bounds__(256) void kv_append_i8_row_kernel(AppendI8Args a) {
+  constexpr int LR = DH / 8, HPW = 64 / LR;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int head = (blockIdx.y * 4 + wave) * HPW + lane / LR, d0 = (lane % LR) * 8;
+  const int which = blockIdx.z, i = blockIdx.x;
+  const int sid = a.at.seq_ids ? a.at.seq_ids[i] : i;
+  const int p_i = a.at.pos ? a.at.pos[i] : 0;
+  if (p_i < 0 || (blockIdx.y * 4 + wave) * HPW >= a.nh) return;
+  const int page = page_at(a.at, sid, p_i >> 6);
+  if (page < 0) return;
+  const int64_t ph = (int64_t)page * a.nh + head;
+  int8_t* codes = a.codes[which] + ph * (FG_PAGE_ROWS * DH);
+  float* scale = a.scales[which] + ph;
+  auto store = [&](int j, int r) {
+    if (head >= a.nh) return;
+    const h8_t x = *reinterpret_cast<const h8_t*>(a.src[which] + (int64_t)j * a.ld + (int64_t)head * DH + d0);
+    const float was = r > 0 ? *scale : 0.f;
+    float top = abs_max(x, 0.f);   // over the head's lanes
+    top = fmaxf(top, dpp_f32<kDppXor1>(top));
+    top = fmaxf(top, dpp_f32<kDppXor2>(top));
+    top = fmaxf(top, dpp_f32<kDppHalfMirror>(top));
+    if (LR == 16) top = fmaxf(top, dpp_f32<kDppMirror>(top));
+    const Step st = step_of(top, was, r > 0);
+    i8x8_t c;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) c[e] = code_of(x[e], st);
+    if (st.grown) {
+      if (which == 0) {
+        for (int n = 0; n < FG_PAGE_ROWS; ++n) {
+          i8x8_t* dst = reinterpret_cast<i8x8_t*>(codes + n * DH + d0);
+          i8x8_t old = *dst;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) old[e] = again(old[e], st);
+          *dst = old;
+        }
+      } else {
+        for (int n = 0; n < FG_PAGE_ROWS / 2; ++n) {   // eight dimensions' units of four groups
+          i8x8_t* dst = reinterpret_cast<i8x8_t*>(codes + ((n >> 3) * DH + d0 + (n & 7)) * 16);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            i8x8_t old = dst[h];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) old[e] = again(old[e], st);
+            dst[h] = old;
+          }
+        }
+      }
+    }
+    if (which == 0) {
+      *reinterpret_cast<i8x8_t*>(codes + r * DH + d0) = c;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) codes[((r >> 4) * DH + d0 + e) * 16 + (r & 15)] = c[e];
+    }
+    if (d0 == 0) *scale = st.now;
+  };
+  if (!a.at.seq_ids) {
+    store(i, p_i & 63);
+    return;
+  }
+  for (int base = 0; base < a.b; base += 64) {   // as above
+    const int j = base + lane;
+    int p = -1;
+    if (j < a.b && a.at.seq_ids[j] == sid) p = a.at.pos ? a.at.pos[j] : 0;
+    uint64_t m = __builtin_amdgcn_ballot_w64(p >= 0 && p >> 6 == p_i >> 6);
+    while (m) {
+      const int l = __builtin_ctzll(m);
+      m &= m - 1;
+      if (base + l < i) return;
+      store(base + l, __builtin_amdgcn_readlane(p, l) & 63);
+      __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+    }
+  }
+}
+
 // Rounded to binary32 first, as fg_dequantize_groupwise returns it: without the empty statement the compiler may turn an
 // FMA and the conversion behind it into one instruction that rounds once.
 __device__ __forceinline__ half_t to_half(float y) {
@@ -164,53 +278,108 @@ struct GatherArgs {
   const void* meta[2];
   half_t* out[2];
   int64_t ld;
-  int32_t b, s, nh, dtype;
+  int32_t b, s, nh, slots, head_groups;
   PageRows at;
 };
 
-// One thread per 8 head dimensions of one row of one head.
-template <int DH>
+// One wave per (sequence of the call, page, head, K or V), four groups of 16 positions one after the other; lane = 8 head
+// dimensions (lane % LR) of RPL positions of the group.  All loads go out before the first value is used, and groups that
+// nobody asked for are skipped.  The 8-bit value codes come in their units, in order, and pass through LDS.
+template <int DH, int FMT>
 __global__ __launch_bounds__(256) void kv_gather_kernel(GatherArgs a) {
-  constexpr int C = DH / 8;
+  constexpr int LR = DH / 8, RPL = LR / 4, UPL = DH / 64;   // positions of a group, units of a group per lane
+  constexpr bool I8 = FMT == FG_I8P64, H16 = FMT == FG_Q4G64_H16;
+  __shared__ __attribute__((aligned(16))) uint8_t sm[I8 ? 4 : 1][I8 ? 16 * DH : 16];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int unit = blockIdx.x / a.head_groups, head = (blockIdx.x - unit * a.head_groups) * 4 + wave;
+  if (head >= a.nh) return;
   const int which = blockIdx.y;
-  const int64_t n = (int64_t)a.b * a.s * a.nh * C;
-  for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < n; t += (int64_t)gridDim.x * 256) {
-    const int d0 = (int)(t % C) * 8;
-    const int64_t u = t / C;
-    const int head = (int)(u % a.nh);
-    const int64_t row = u / a.nh;
-    const int i = (int)(row / a.s), j = (int)(row - (int64_t)i * a.s);
-    const int64_t p = (int64_t)(a.at.pos ? a.at.pos[i] : 0) + j;
-    const int page = p < 0 ? -1 : page_at(a.at, a.at.seq_ids ? a.at.seq_ids[i] : i, p >> 6);
-    h8_t v = (h8_t)(half_t)0;
-    if (page >= 0) {
-      const int r = (int)(p & 63);
-      const int64_t ph = (int64_t)page * a.nh + head, prow = ph * FG_PAGE_ROWS + r;
-      if (a.dtype == FG_F16) {
-        v = *reinterpret_cast<const h8_t*>(reinterpret_cast<const half_t*>(a.codes[which]) + prow * DH + d0);
-      } else if (a.dtype == FG_I8P64) {
-        const int8_t* c = reinterpret_cast<const int8_t*>(a.codes[which]) + ph * (FG_PAGE_ROWS * DH);
-        const float sc = reinterpret_cast<const float*>(a.meta[which])[ph];
+  const int i = unit / a.slots, k = unit - i * a.slots;
+  const int64_t p_i = a.at.pos ? a.at.pos[i] : 0;
+  const int64_t slot = (p_i >> 6) + k, s0 = slot << 6;
+  if (s0 >= p_i + a.s) return;
+  const int page = page_at(a.at, a.at.seq_ids ? a.at.seq_ids[i] : i, slot);
+  const int lo = p_i > s0 ? (int)(p_i - s0) : 0, hi = p_i + a.s < s0 + 64 ? (int)(p_i + a.s - s0) : 64;
+  const int d0 = (lane % LR) * 8, r0 = (lane / LR) * RPL;
+  half_t* out = a.out[which] + ((int64_t)i * a.s + (s0 - p_i)) * a.ld + (int64_t)head * DH + d0;   // of the page's row 0
+  auto put = [&](int row, const h8_t v) {
+    if (row >= lo && row < hi) *reinterpret_cast<h8_t*>(out + (int64_t)row * a.ld) = v;
+  };
+  if (page < 0) {
+    for (int q = 0; q < 4; ++q)
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          v[e] = to_half((float)c[which ? ((r >> 4) * DH + d0 + e) * 16 + (r & 15) : r * DH + d0 + e] * sc);
-      } else {
-        const uint32_t c = *reinterpret_cast<const uint32_t*>(reinterpret_cast<const uint8_t*>(a.codes[which]) + (prow * DH + d0) / 2);
-        const int64_t g = (prow * DH + d0) / kGroup;
-        float mn, sc;
-        if (a.dtype == FG_Q4G64_H16) {
-          const h2_t m = reinterpret_cast<const h2_t*>(a.meta[which])[g];
-          mn = (float)m.x, sc = (float)m.y;
-        } else {
-          const float2 m = reinterpret_cast<const float2*>(a.meta[which])[g];
-          mn = m.x, sc = m.y;
+      for (int n = 0; n < RPL; ++n) put(16 * q + r0 + n, (h8_t)(half_t)0);
+    return;
+  }
+  auto wanted = [&](int q) { return 16 * q < hi && 16 * q + 16 > lo; };   // the same in all lanes
+  const int64_t ph = (int64_t)page * a.nh + head;
+  if (I8 && which) {
+    const uint8_t* codes = reinterpret_cast<const uint8_t*>(a.codes[1]) + ph * (FG_PAGE_ROWS * DH);
+    const float sc = reinterpret_cast<const float*>(a.meta[1])[ph];
+    u4_t u[4][UPL];
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (wanted(q))
+#pragma unroll
+        for (int t = 0; t < UPL; ++t) u[q][t] = *reinterpret_cast<const u4_t*>(codes + (q * DH + 64 * t + lane) * 16);
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (wanted(q)) {
+        wave_lds_fence();
+#pragma unroll
+        for (int t = 0; t < UPL; ++t) *reinterpret_cast<u4_t*>(sm[wave] + unit_at<DH>(0, 64 * t + lane)) = u[q][t];
+        wave_lds_fence();
+        uint32_t c[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const uint8_t* from = sm[wave] + unit_at<DH>(0, d0 + e) + r0;
+          c[e] = RPL == 4 ? *reinterpret_cast<const uint32_t*>(from) : *reinterpret_cast<const uint16_t*>(from);
         }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = to_half(__builtin_fmaf((float)((c >> (4 * e)) & 15u), sc, mn));
+        for (int n = 0; n < RPL; ++n) {
+          h8_t v;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = to_half((float)(int8_t)(c[e] >> (8 * n)) * sc);
+          put(16 * q + r0 + n, v);
+        }
       }
-    }
-    *reinterpret_cast<h8_t*>(a.out[which] + row * a.ld + head * DH + d0) = v;
+    return;
   }
+  // rows in the order of their positions: raw[] = the lane's 8 elements as stored
+  using raw_t = std::conditional_t<FMT == FG_F16, h8_t, std::conditional_t<I8, i8x8_t, uint32_t>>;
+  using meta_t = std::conditional_t<H16, h2_t, float2>;
+  const raw_t* rows = reinterpret_cast<const raw_t*>(a.codes[which]) + ph * FG_PAGE_ROWS * LR + lane % LR;
+  const float sc = I8 ? reinterpret_cast<const float*>(a.meta[which])[ph] : 0.f;
+  raw_t raw[4][RPL];
+  meta_t pair[4][FMT == FG_F16 || I8 ? 1 : RPL];
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+    if (wanted(q))
+#pragma unroll
+      for (int n = 0; n < RPL; ++n) {
+        const int row = 16 * q + r0 + n;
+        raw[q][n] = rows[row * LR];
+        if constexpr (FMT == FG_Q4G64 || H16)
+          pair[q][n] = reinterpret_cast<const meta_t*>(a.meta[which])[(ph * FG_PAGE_ROWS + row) * (DH / kGroup) + d0 / kGroup];
+      }
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+    if (wanted(q))
+#pragma unroll
+      for (int n = 0; n < RPL; ++n) {
+        h8_t v;
+        if constexpr (FMT == FG_F16) {
+          v = raw[q][n];
+        } else if constexpr (I8) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = to_half((float)raw[q][n][e] * sc);
+        } else {
+          const float mn = (float)pair[q][n].x, step = (float)pair[q][n].y;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = to_half(__builtin_fmaf((float)((raw[q][n] >> (4 * e)) & 15u), step, mn));
+        }
+        put(16 * q + r0 + n, v);
+      }
 }
 
 }  // namespace
@@ -235,11 +404,24 @@ int kv_append_i8_launch(const fg_model_cfg& cfg, const half_t* k, const half_t* 
   a.nh = cfg.nh;
   a.slots = use_pos && seqs.pos ? (int)ceil_div((int64_t)s + 63, 64) : (int)ceil_div(s, 64);
   a.at = page_rows(pages, seqs, use_pos);
-  const int64_t units = (int64_t)b * a.slots;
-  if (units > 0x7fffffff || ceil_div(cfg.nh, 4) > 65535) return FG_ERR_SHAPE;
-  const dim3 grid((unsigned)units, (unsigned)ceil_div(cfg.nh, 4), 2);
+  const int dh = cfg.h1 / cfg.nh;
   ProfScope prof(FG_K_KV_APPEND, stream);
-  if (cfg.h1 / cfg.nh == 128)
+  if (s == 1) {
+    const int hpw = 512 / dh;   // heads a wave
+    if (ceil_div(cfg.nh, 4 * hpw) > 65535) return FG_ERR_SHAPE;
+    const dim3 grid((unsigned)b, (unsigned)ceil_div(cfg.nh, 4 * hpw), 2);
+    if (dh == 128)
+      hipLaunchKernelGGL(kv_append_i8_row_kernel<128>, grid, dim3(256), 0, stream, a);
+    else
+      hipLaunchKernelGGL(kv_append_i8_row_kernel<64>, grid, dim3(256), 0, stream, a);
+    FG_LAUNCH_CHECK();
+    return FG_OK;
+  }
+  a.head_groups = (int)ceil_div(cfg.nh, 4);
+  const int64_t blocks = (int64_t)b * a.slots * a.head_groups;
+  if (blocks > 0x7fffffff) return FG_ERR_SHAPE;
+  const dim3 grid((unsigned)blocks, 2);
+  if (dh == 128)
     hipLaunchKernelGGL(kv_append_i8_kernel<128>, grid, dim3(256), 0, stream, a);
   else
     hipLaunchKernelGGL(kv_append_i8_kernel<64>, grid, dim3(256), 0, stream, a);
@@ -273,16 +455,30 @@ extern "C" int fg_kv_gather_paged(const fg_model_cfg* cfg, const fg_kv_pages* pa
   a.b = b;
   a.s = s;
   a.nh = cfg->nh;
-  a.dtype = pages->dtype;
   a.at = page_rows(*pages, *seqs, true);
-  const int64_t blocks = ceil_div((int64_t)b * s * cfg->h1 / 8, 256);
-  const dim3 grid((unsigned)(blocks < 16384 ? blocks : 16384), 2);
+  a.slots = seqs->pos ? (int)ceil_div((int64_t)s + 63, 64) : (int)ceil_div(s, 64);
+  a.head_groups = (int)ceil_div(cfg->nh, 4);
+  const int64_t blocks = (int64_t)b * a.slots * a.head_groups;
+  if (blocks > 0x7fffffff) return FG_ERR_SHAPE;
+  const dim3 grid((unsigned)blocks, 2);
   hipStream_t st = as_stream(stream);
   ProfScope prof(FG_K_KV_GATHER, st);
-  if (cfg->h1 / cfg->nh == 128)
-    hipLaunchKernelGGL(kv_gather_kernel<128>, grid, dim3(256), 0, st, a);
+#define FG_GATHER(FMT_)                                                                        \
+  do {                                                                                         \
+    if (cfg->h1 / cfg->nh == 128)                                                              \
+      hipLaunchKernelGGL((kv_gather_kernel<128, FMT_>), grid, dim3(256), 0, st, a);            \
+    else                                                                                       \
+      hipLaunchKernelGGL((kv_gather_kernel<64, FMT_>), grid, dim3(256), 0, st, a);             \
+  } while (0)
+  if (pages->dtype == FG_I8P64)
+    FG_GATHER(FG_I8P64);
+  else if (pages->dtype == FG_F16)
+    FG_GATHER(FG_F16);
+  else if (pages->dtype == FG_Q4G64_H16)
+    FG_GATHER(FG_Q4G64_H16);
   else
-    hipLaunchKernelGGL(kv_gather_kernel<64>, grid, dim3(256), 0, st, a);
+    FG_GATHER(FG_Q4G64);
+#undef FG_GATHER
   FG_LAUNCH_CHECK();
   return FG_OK;
 }
