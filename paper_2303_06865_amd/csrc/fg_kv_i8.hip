@@ -52,12 +52,34 @@ __device__ __forceinline__ Step step_of(float top, float old, bool begun) {
   s.inv = s.now > 0.f ? 1.0f / s.now : 0.f;
   return s;
 }
-__device__ __forceinline__ int8_t code_of(half_t v, const Step& s) { return (int8_t)(int)rintf((float)v * s.inv); }
-__device__ __forceinline__ int8_t again(int8_t c, const Step& s) { return (int8_t)(int)rintf((float)c * s.ratio); }
-__device__ __forceinline__ float abs_max(const h8_t v, float top) {
+// rint in one addition: 1.5 * 2^23 + y has the whole number in its low bits, two's complement (the code is the lowest byte)
+__device__ __forceinline__ uint32_t whole(float y) { return __builtin_bit_cast(uint32_t, y + 12582912.0f); }
+// (the FMA with nothing is the product, rounded once, taken from FP16 as it is)
+__device__ __forceinline__ uint32_t code_of(half_t v, const Step& s) { return whole(__builtin_fmaf((float)v, s.inv, 0.f)); }
+__device__ __forceinline__ uint32_t again(int8_t c, const Step& s) { return whole((float)c * s.ratio); }
+__device__ __forceinline__ uint32_t bytes4(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {   // their lowest bytes
+  return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0c0c0400u), __builtin_amdgcn_perm(b, a, 0x0c0c0400u), 0x05040100u);
+}
+// magnitudes of FP16 numbers are ordered as their bits without the sign
+typedef uint16_t us8_t __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ us8_t abs_max(const h8_t v, us8_t top) {
+  return __builtin_elementwise_max(__builtin_bit_cast(us8_t, v) & (us8_t)(uint16_t)0x7fff, top);
+}
+__device__ __forceinline__ float largest(us8_t t) {
+  const uint16_t a = __builtin_elementwise_max(__builtin_elementwise_max(t[0], t[1]), __builtin_elementwise_max(t[2], t[3]));
+  const uint16_t b = __builtin_elementwise_max(__builtin_elementwise_max(t[4], t[5]), __builtin_elementwise_max(t[6], t[7]));
+  return (float)__builtin_bit_cast(half_t, (uint16_t)__builtin_elementwise_max(a, b));
+}
+
+__device__ __forceinline__ u2_t row_codes(const h8_t x, const Step& s) {
+  return (u2_t){bytes4(code_of(x[0], s), code_of(x[1], s), code_of(x[2], s), code_of(x[3], s)),
+                bytes4(code_of(x[4], s), code_of(x[5], s), code_of(x[6], s), code_of(x[7], s))};
+}
+__device__ __forceinline__ u2_t codes_again(u2_t c, const Step& s) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf((float)v[e]));
-  return top;
+  for (int w = 0; w < 2; ++w)
+    c[w] = bytes4(again((int8_t)c[w], s), again((int8_t)(c[w] >> 8), s), again((int8_t)(c[w] >> 16), s), again((int8_t)(c[w] >> 24), s));
+  return c;
 }
 
 // The units of 16 positions of a page's value codes in LDS, [group of 16][dh] in an order in which the lanes that hold eight
@@ -67,74 +89,79 @@ __device__ __forceinline__ int unit_at(int group, int d) {
   return (group * DH + (d & ~7) + (((d & 7) + (d >> 3)) & 7)) * 16;
 }
 
-// One wave per (sequence of the call, page it touches, head, K or V).  Lane = 8 head dimensions (lane % LR) of NR
-// consecutive positions (lane / LR): a row of a head is read by LR lanes, 16 bytes each, and at head size 128 the
-// lane's 16 positions are one unit of the value codes' order.  Values go through LDS, so that their units leave in order (straight
-// from the lanes, 16 bytes in every 128, 16 x 500 rows of 32 heads took 70 us instead of ~).
+// One wave per (sequence of the call, page it touches, head, K or V), in four groups of 16 positions; lane = 8 head dimensions
+// (lane % LR) of RPL positions of each group.  The page's new rows stay in registers until their largest magnitude is known.
+// Value codes pass through LDS and leave in their units, in order (straight from the lanes, 16 bytes in every 128, storing
+// 16 x 500 rows of 32 heads took 70 us).
 template <int DH, bool VALUES>
 __device__ __forceinline__ void store_rows(const half_t* src, int64_t ld, int8_t* codes, float* scale, int lo, int hi, int lane,
                                            uint8_t* sm) {
-  constexpr int LR = DH / 8, NR = LR;   // 64 positions over 64 / LR groups of lanes
-  const int d0 = (lane % LR) * 8, r0 = (lane / LR) * NR;
+  constexpr int LR = DH / 8, RPL = LR / 4, UPL = DH / 64;   // positions of a group, units of a group per lane
+  __asm__ volatile("" : "+v"(lane));   // addresses are made here, not kept in registers from before the caller's loop
+  const int d0 = (lane % LR) * 8, r0 = (lane / LR) * RPL;
   const float was = lo > 0 ? *scale : 0.f;
-  h8_t x[NR];
+  h8_t x[4][RPL];
 #pragma unroll
-  for (int n = 0; n < NR; ++n) {
-    x[n] = (h8_t)(half_t)0;
-    if (r0 + n >= lo && r0 + n < hi) x[n] = *reinterpret_cast<const h8_t*>(src + (int64_t)(r0 + n - lo) * ld + d0);
-  }
-  float top = 0.f;
+  for (int q = 0; q < 4; ++q)
 #pragma unroll
-  for (int n = 0; n < NR; ++n) top = abs_max(x[n], top);
-  const Step st = step_of(wave_max(top), was, lo > 0);   // the same in all lanes
-  if constexpr (!VALUES) {
+    for (int n = 0; n < RPL; ++n) {
+      int row = 16 * q + r0 + n;
+      row = row < lo ? lo : (row < hi ? row : hi - 1);   // a new row again in the place of one that is not: the largest stays
+      x[q][n] = *reinterpret_cast<const h8_t*>(src + (int64_t)(row - lo) * ld + d0);
+    }
+  us8_t top = (us8_t)(uint16_t)0;
 #pragma unroll
-    for (int n = 0; n < NR; ++n) {
-      const int r = r0 + n;
-      i8x8_t* dst = reinterpret_cast<i8x8_t*>(codes + r * DH + d0);
-      const bool fresh = r >= lo && r < hi;
-      if (fresh || st.grown) {
-        i8x8_t c;
-        if (fresh) {
+  for (int q = 0; q < 4; ++q)
 #pragma unroll
-          for (int e = 0; e < 8; ++e) c[e] = code_of(x[n][e], st);
-        } else {
-          const i8x8_t old = *dst;
+    for (int n = 0; n < RPL; ++n) top = abs_max(x[q][n], top);
+  const Step st = step_of(wave_max(largest(top)), was, lo > 0);   // the same in all lanes
 #pragma unroll
-          for (int e = 0; e < 8; ++e) c[e] = again(old[e], st);
+  for (int q = 0; q < 4; ++q) {
+    __builtin_amdgcn_sched_barrier(0);   // one group's codes at a time in registers
+    if (!(st.grown || (16 * q < hi && 16 * q + 16 > lo))) continue;
+    if constexpr (!VALUES) {
+#pragma unroll
+      for (int n = 0; n < RPL; ++n) {
+        const int row = 16 * q + r0 + n;
+        u2_t* dst = reinterpret_cast<u2_t*>(codes + row * DH + d0);
+        if (row >= lo && row < hi)
+          *dst = row_codes(x[q][n], st);
+        else if (st.grown)
+          *dst = codes_again(*dst, st);
+      }
+    } else {
+      wave_lds_fence();   // what was read from there before has been
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        uint8_t* to = sm + unit_at<DH>(0, d0 + e) + r0;
+        const uint32_t c0 = code_of(x[q][0][e], st), c1 = code_of(x[q][1][e], st);
+        if constexpr (RPL == 4)
+          *reinterpret_cast<uint32_t*>(to) = bytes4(c0, c1, code_of(x[q][2][e], st), code_of(x[q][3][e], st));
+        else
+          *reinterpret_cast<uint16_t*>(to) = (uint16_t)__builtin_amdgcn_perm(c1, c0, 0x0c0c0400u);
+      }
+      wave_lds_fence();
+      const bool whole = 16 * q >= lo && 16 * q + 16 <= hi;
+#pragma unroll
+      for (int t = 0; t < UPL; ++t) {
+        u4_t* dst = reinterpret_cast<u4_t*>(codes + (q * DH + 64 * t + lane) * 16);
+        u4_t c = *reinterpret_cast<const u4_t*>(sm + unit_at<DH>(0, 64 * t + lane));
+        if (!whole) {   // the unit's other positions stay, in the page's new step
+          const u4_t old = *dst;
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            uint32_t m = 0;
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+              const int row = 16 * q + 4 * w + n;
+              const int8_t o = (int8_t)(old[w] >> (8 * n));
+              const uint32_t v = row >= lo && row < hi ? c[w] >> (8 * n) : (st.grown ? again(o, st) : (uint32_t)o);
+              m |= (v & 255u) << (8 * n);
+            }
+            c[w] = m;
+          }
         }
         *dst = c;
-      }
-    }
-  } else {
-    const bool any = r0 < hi && r0 + NR > lo, all = r0 >= lo && r0 + NR <= hi;
-    wave_lds_fence();   // what was read from there before has been
-    if (any || st.grown) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-#pragma unroll
-        for (int n8 = 0; n8 < NR / 8; ++n8) {
-          const int r = r0 + 8 * n8;
-          i8x8_t c = (i8x8_t)(int8_t)0;
-          if (!all) c = *reinterpret_cast<const i8x8_t*>(codes + ((r >> 4) * DH + d0 + e) * 16 + (r & 15));
-#pragma unroll
-          for (int n = 0; n < 8; ++n)
-            c[n] = r + n >= lo && r + n < hi ? code_of(x[8 * n8 + n][e], st) : (st.grown ? again(c[n], st) : c[n]);
-          *reinterpret_cast<i8x8_t*>(sm + unit_at<DH>(r >> 4, d0 + e) + (r & 15)) = c;
-        }
-    }
-    wave_lds_fence();
-#pragma unroll
-    for (int i = 0; i < DH / 16; ++i) {
-      const int u = 64 * i + lane, group = u / DH, d = u % DH;
-      // (at head size 64 a group of 16 positions is two lanes' work: a half that is not new is kept)
-      const bool lower = st.grown || (16 * group < hi && 16 * group + 8 > lo), upper = st.grown || (16 * group + 8 < hi && 16 * group + 16 > lo);
-      const uint8_t* from = sm + unit_at<DH>(group, d);
-      if (NR == 16 ? lower || upper : lower && upper) {
-        *reinterpret_cast<u4_t*>(codes + u * 16) = *reinterpret_cast<const u4_t*>(from);
-      } else if (NR == 8 && (lower || upper)) {
-        const int h = lower ? 0 : 8;
-        *reinterpret_cast<u2_t*>(codes + u * 16 + h) = *reinterpret_cast<const u2_t*>(from + h);
       }
     }
   }
@@ -142,8 +169,8 @@ __device__ __forceinline__ void store_rows(const half_t* src, int64_t ld, int8_t
 }
 
 template <int DH>
-__global__ __launch_bounds__(256) void kv_append_i8_kernel(AppendI8Args a) {
-  __shared__ __attribute__((aligned(16))) uint8_t sm[4][FG_PAGE_ROWS * DH];
+__global__ __launch_bounds__(256, 4) void kv_append_i8_kernel(AppendI8Args a) {
+  __shared__ __attribute__((aligned(16))) uint8_t sm[4][16 * DH];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int unit = blockIdx.x / a.head_groups, head = (blockIdx.x - unit * a.head_groups) * 4 + wave;
   if (head >= a.nh) return;
@@ -168,15 +195,12 @@ __global__ __launch_bounds__(256) void kv_append_i8_kernel(AppendI8Args a) {
     else
       store_rows<DH, true>(src, a.ld, codes, scale, lo, hi, lane, sm[wave]);
   };
-  if (!a.at.seq_ids) {
-    store(i, p_i);
-    return;
-  }
   // A sequence that is named more than once: the first of its rows that touches the page stores them all, in order.
-  for (int base = 0; base < a.b; base += 64) {
+  const int from = a.at.seq_ids ? 0 : i, to = a.at.seq_ids ? a.b : i + 1;
+  for (int base = from; base < to; base += 64) {
     const int j = base + lane;
     int64_t p = -1;
-    if (j < a.b && a.at.seq_ids[j] == sid) p = a.at.pos ? a.at.pos[j] : 0;
+    if (j < to && (!a.at.seq_ids || a.at.seq_ids[j] == sid)) p = a.at.pos ? a.at.pos[j] : 0;
     uint64_t m = __builtin_amdgcn_ballot_w64(p >= 0 && p < s0 + 64 && p + a.s > s0);
     while (m) {
       const int l = __builtin_ctzll(m);
@@ -208,42 +232,23 @@ __global__ __launch_bounds__(256) void kv_append_i8_row_kernel(AppendI8Args a) {
     if (head >= a.nh) return;
     const h8_t x = *reinterpret_cast<const h8_t*>(a.src[which] + (int64_t)j * a.ld + (int64_t)head * DH + d0);
     const float was = r > 0 ? *scale : 0.f;
-    float top = abs_max(x, 0.f);   // over the head's lanes
+    float top = largest(abs_max(x, (us8_t)(uint16_t)0));   // and over the head's lanes
     top = fmaxf(top, dpp_f32<kDppXor1>(top));
     top = fmaxf(top, dpp_f32<kDppXor2>(top));
     top = fmaxf(top, dpp_f32<kDppHalfMirror>(top));
     if (LR == 16) top = fmaxf(top, dpp_f32<kDppMirror>(top));
     const Step st = step_of(top, was, r > 0);
-    i8x8_t c;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) c[e] = code_of(x[e], st);
-    if (st.grown) {
-      if (which == 0) {
-        for (int n = 0; n < FG_PAGE_ROWS; ++n) {
-          i8x8_t* dst = reinterpret_cast<i8x8_t*>(codes + n * DH + d0);
-          i8x8_t old = *dst;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) old[e] = again(old[e], st);
-          *dst = old;
-        }
-      } else {
-        for (int n = 0; n < FG_PAGE_ROWS / 2; ++n) {   // eight dimensions' units of four groups
-          i8x8_t* dst = reinterpret_cast<i8x8_t*>(codes + ((n >> 3) * DH + d0 + (n & 7)) * 16);
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            i8x8_t old = dst[h];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) old[e] = again(old[e], st);
-            dst[h] = old;
-          }
-        }
+    const u2_t c = row_codes(x, st);
+    if (st.grown)   // K: 64 rows; V: the units of eight dimensions in four groups, in halves
+      for (int n = 0; n < FG_PAGE_ROWS; ++n) {
+        u2_t* dst = reinterpret_cast<u2_t*>(codes + (which == 0 ? n * DH + d0 : ((n >> 4) * DH + d0 + (n >> 1 & 7)) * 16 + (n & 1) * 8));
+        *dst = codes_again(*dst, st);
       }
-    }
     if (which == 0) {
-      *reinterpret_cast<i8x8_t*>(codes + r * DH + d0) = c;
+      *reinterpret_cast<u2_t*>(codes + r * DH + d0) = c;
     } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) codes[((r >> 4) * DH + d0 + e) * 16 + (r & 15)] = c[e];
+      for (int e = 0; e < 8; ++e) codes[((r >> 4) * DH + d0 + e) * 16 + (r & 15)] = (int8_t)(c[e >> 2] >> (8 * (e & 3)));
     }
     if (d0 == 0) *scale = st.now;
   };
