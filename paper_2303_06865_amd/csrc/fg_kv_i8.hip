@@ -172,9 +172,9 @@ template <int DH>
 __global__ __launch_bounds__(256, 4) void kv_append_i8_kernel(AppendI8Args a) {
   __shared__ __attribute__((aligned(16))) uint8_t sm[4][16 * DH];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int unit = blockIdx.x / a.head_groups, head = (blockIdx.x - unit * a.head_groups) * 4 + wave;
+  const int both = blockIdx.x / a.head_groups, head = (blockIdx.x - both * a.head_groups) * 4 + wave;
   if (head >= a.nh) return;
-  const int which = blockIdx.y;
+  const int unit = both >> 1, which = both & 1;   // K and V next to each other, as they lie in the projection's rows
   const int i = unit / a.slots, k = unit - i * a.slots;
   const int sid = a.at.seq_ids ? a.at.seq_ids[i] : i;
   const int64_t p_i = a.at.pos ? a.at.pos[i] : 0;
@@ -423,9 +423,9 @@ int kv_append_i8_launch(const fg_model_cfg& cfg, const half_t* k, const half_t* 
     return FG_OK;
   }
   a.head_groups = (int)ceil_div(cfg.nh, 4);
-  const int64_t blocks = (int64_t)b * a.slots * a.head_groups;
+  const int64_t blocks = (int64_t)b * a.slots * a.head_groups * 2;
   if (blocks > 0x7fffffff) return FG_ERR_SHAPE;
-  const dim3 grid((unsigned)blocks, 2);
+  const dim3 grid((unsigned)blocks);
   if (dh == 128)
     hipLaunchKernelGGL(kv_append_i8_kernel<128>, grid, dim3(256), 0, stream, a);
   else
