@@ -362,24 +362,37 @@ __global__ __launch_bounds__(256) void attn_decode_i8_kernel(AttnI8Args a) {
   }
 }
 
-// One wave per (row, query head): the splits' partial results together.
+// One workgroup per (row, query head): the splits' partial results together, a quarter of them per wave.
+constexpr int kMostSplits = 64;
 template <int DH>
-__global__ __launch_bounds__(256) void attn_merge_i8_kernel(AttnI8Args a, int64_t n) {
-  const int lane = threadIdx.x & 63;
-  const int64_t rh = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (rh >= n) return;
-  const float2* ml = a.part_ml + rh * a.splits;
-  float M = -INFINITY;
-  for (int s = 0; s < a.splits; ++s) M = fmaxf(M, ml[s].x);
-  float den = 0.f, num[DH / 64] = {};
-  for (int s = 0; s < a.splits; ++s) {
-    const float f = ml[s].x == -INFINITY ? 0.f : fast_exp2(ml[s].x - M);
-    den += f * ml[s].y;
+__global__ __launch_bounds__(256) void attn_merge_i8_kernel(AttnI8Args a) {
+  constexpr int N = DH / 64, PER = kMostSplits / 4;
+  __shared__ float sm[4][DH];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t rh = blockIdx.x, p0 = rh * a.splits;
+  const float2 ml = lane < a.splits ? a.part_ml[p0 + lane] : make_float2(-INFINITY, 0.f);
+  float v[PER][N];
 #pragma unroll
-    for (int k = 0; k < DH / 64; ++k) num[k] += f * a.part_o[(rh * a.splits + s) * DH + lane + 64 * k];
-  }
+  for (int i = 0; i < PER; ++i)
+    if (4 * i + wave < a.splits)
 #pragma unroll
-  for (int k = 0; k < DH / 64; ++k) a.out[rh * DH + lane + 64 * k] = (half_t)(den > 0.f ? num[k] / den : 0.f);
+      for (int k = 0; k < N; ++k) v[i][k] = a.part_o[(p0 + 4 * i + wave) * DH + lane + 64 * k];
+  const float M = wave_max(ml.x);
+  const float f = ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - M);
+  const float den = wave_sum(f * ml.y);
+  float num[N] = {};
+#pragma unroll
+  for (int i = 0; i < PER; ++i)
+    if (4 * i + wave < a.splits) {
+      const float fi = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), 4 * i + wave));
+#pragma unroll
+      for (int k = 0; k < N; ++k) num[k] = __builtin_fmaf(fi, v[i][k], num[k]);
+    }
+#pragma unroll
+  for (int k = 0; k < N; ++k) sm[wave][lane + 64 * k] = num[k];
+  __syncthreads();
+  const int d = threadIdx.x;
+  if (d < DH) a.out[rh * DH + d] = (half_t)(den > 0.f ? (sm[0][d] + sm[1][d] + sm[2][d] + sm[3][d]) / den : 0.f);
 }
 
 struct Plan {
@@ -397,7 +410,7 @@ Plan plan_i8(int32_t nh, int32_t nkv, int32_t beams, int32_t b, int32_t table_st
   p.wpu = p.units >= 2048 ? 1 : (p.units >= 1024 ? 2 : 4);
   const int64_t want = ceil_div(1024, p.units), most = ceil_div(table_stride, 8);   // two pages a wave at least
   p.splits = p.wpu < 4 ? 1 : (int)(want < most ? want : most);
-  if (p.splits > 128) p.splits = 128;
+  if (p.splits > kMostSplits) p.splits = kMostSplits;
   if (p.splits < 1) p.splits = 1;
   return p;
 }
@@ -465,11 +478,10 @@ int decode_attention_i8_launch(const fg_model_cfg& cfg, int32_t nkv, int32_t bea
 #undef FG_I8
   FG_LAUNCH_CHECK();
   if (p.splits > 1) {
-    const dim3 mg((unsigned)ceil_div(rh, 4));
     if (dh == 128)
-      hipLaunchKernelGGL(attn_merge_i8_kernel<128>, mg, dim3(256), 0, stream, a, rh);
+      hipLaunchKernelGGL(attn_merge_i8_kernel<128>, dim3((unsigned)rh), dim3(256), 0, stream, a);
     else
-      hipLaunchKernelGGL(attn_merge_i8_kernel<64>, mg, dim3(256), 0, stream, a, rh);
+      hipLaunchKernelGGL(attn_merge_i8_kernel<64>, dim3((unsigned)rh), dim3(256), 0, stream, a);
     FG_LAUNCH_CHECK();
   }
   return FG_OK;

@@ -383,36 +383,36 @@ __global__ __launch_bounds__(256) void beam_table_kernel(ReorderArgs a) {
     }
   }
   __syncthreads();
-  if (tid == 0) {
-    int next = 0, miss = 0;
-    for (int j = 0; j < a.beams; ++j) {
-      const int n = rows_of(j), slot = n >> 6;
-      a.pos_out[row0 + j] = raw[j];
-      int2 cp = make_int2(-1, -1);
-      const bool begun = (n & 63) != 0;
-      bool takes = slot < a.stride;
-      if (begun) {
-        const int pg = last[j];
-        bool mine = pg >= first && pg - first < a.per_group;
-        for (int k = 0; k < j; ++k) mine = mine && !(last[k] == pg && (rows_of(k) & 63) != 0);
-        takes = takes && !mine;
-      }
-      if (slot >= a.stride) ++miss;
-      if (takes) {
-        while (next < a.per_group && (held[next >> 5] >> (next & 31)) & 1) ++next;
-        int pg = -1;
-        if (next < a.per_group)
-          pg = first + next++;
-        else
-          ++miss;
-        a.table_out[(row0 + j) * a.stride + slot] = pg;
-        if (begun && pg >= 0 && last[j] >= 0 && last[j] < a.n_pages) cp = make_int2(last[j], pg);
-      }
-      a.copies[row0 + j] = cp;
-      a.filled[row0 + j] = ((n & 63) + 15) & ~15;
+  if (tid >= 64) return;
+  // lane = beam: does it take a page of its own, and the how many-th of those that do
+  const int n = tid < a.beams ? rows_of(tid) : 0, slot = n >> 6;
+  const bool begun = (n & 63) != 0, fits = tid < a.beams && slot < a.stride;
+  const int was = tid < a.beams ? last[tid] : -1;
+  bool keeps = begun && was >= first && was - first < a.per_group;
+  for (int k = 0; k < a.beams; ++k) keeps = keeps && !(k < tid && last[k] == was && (rows_of(k) & 63) != 0);
+  const bool takes = fits && !keeps;
+  const uint64_t takers = __builtin_amdgcn_ballot_w64(takes);
+  const int rank = __builtin_popcountll(takers & ((1ull << tid) - 1)), need = __builtin_popcountll(takers);
+  int page = -1, given = 0;
+  for (int w = 0; w < words && given < need; ++w) {   // the lowest pages that nobody holds, a word of 32 at a time
+    uint32_t free = ~held[w];
+    if (32 * w + 32 > a.per_group) free &= (1u << (a.per_group & 31)) - 1;
+    const int n_free = __builtin_popcount(free);
+    if (takes && rank >= given && rank < given + n_free) {
+      for (int skip = rank - given; skip > 0; --skip) free &= free - 1;
+      page = first + 32 * w + __builtin_ctz(free);
     }
-    if (a.missing) a.missing[g] = miss;
+    given += n_free;
   }
+  const uint64_t lost = __builtin_amdgcn_ballot_w64(tid < a.beams && (slot >= a.stride || (takes && page < 0)));
+  if (tid < a.beams) {
+    a.pos_out[row0 + tid] = raw[tid];
+    if (takes) a.table_out[(row0 + tid) * a.stride + slot] = page;
+    const bool copies = takes && begun && page >= 0 && was >= 0 && was < a.n_pages;
+    a.copies[row0 + tid] = copies ? make_int2(was, page) : make_int2(-1, -1);
+    a.filled[row0 + tid] = ((n & 63) + 15) & ~15;
+  }
+  if (tid == 0 && a.missing) a.missing[g] = __builtin_popcountll(lost);
 }
 
 constexpr int kLayersPerLaunch = 64;
@@ -420,27 +420,59 @@ struct CopyArgs {
   void* data[kLayersPerLaunch][4];   // k_codes, v_codes, k_meta, v_meta of every layer
   const int2* copies;
   const int32_t* filled;
-  int32_t nh;
+  int32_t rows, nh, layers;
   int32_t unit[2];                   // bytes of 16 rows of one head: codes, pairs (0: none; -1: one scale per head)
 };
 
-// One workgroup per (row, layer, array): the filled rows of all heads of one page.
+// How many rows take a copy only the device knows.  A fixed number of workgroups collects those rows (1024 at a time) in LDS and
+// shares out what there is to do: one (copy, layer, tensor, head) after the other, up to 8 KiB each.
 __global__ __launch_bounds__(256) void beam_copy_kernel(CopyArgs a) {
-  const int2 cp = a.copies[blockIdx.x];
-  if (cp.x < 0) return;
-  const int which = blockIdx.z, unit = a.unit[which >> 1];
-  char* base = reinterpret_cast<char*>(a.data[blockIdx.y][which]);
-  if (unit < 0) {
-    float* f = reinterpret_cast<float*>(base);
-    for (int h = threadIdx.x; h < a.nh; h += 256) f[(int64_t)cp.y * a.nh + h] = f[(int64_t)cp.x * a.nh + h];
-    return;
-  }
-  const int per_head = unit * 4 / 16, part = unit * (a.filled[blockIdx.x] >> 4) / 16;   // 16-byte pieces
-  const u4_t* src = reinterpret_cast<const u4_t*>(base) + (int64_t)cp.x * a.nh * per_head;
-  u4_t* dst = reinterpret_cast<u4_t*>(base) + (int64_t)cp.y * a.nh * per_head;
-  for (int64_t t = threadIdx.x; t < (int64_t)a.nh * part; t += 256) {
-    const int64_t at = t / part * per_head + t % part;
-    dst[at] = src[at];
+  __shared__ int4 list[1024];
+  __shared__ int waves[4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  for (int r0 = 0; r0 < a.rows; r0 += 1024) {
+    int n = 0;
+    for (int r1 = r0; r1 < r0 + 1024 && r1 < a.rows; r1 += 256) {
+      const int row = r1 + tid;
+      int2 cp = make_int2(-1, -1);
+      if (row < a.rows) cp = a.copies[row];
+      const uint64_t m = __builtin_amdgcn_ballot_w64(cp.x >= 0);
+      if (lane == 0) waves[wave] = __builtin_popcountll(m);
+      __syncthreads();
+      int at = n;
+      for (int w = 0; w < wave; ++w) at += waves[w];
+      if (cp.x >= 0) list[at + __builtin_popcountll(m & ((1ull << lane) - 1))] = make_int4(cp.x, cp.y, a.filled[row], 0);
+      n += waves[0] + waves[1] + waves[2] + waves[3];
+      __syncthreads();
+    }
+    const int per_copy = a.layers * 2 * a.nh, items = n * per_copy;   // below 2^31: see the launch
+    for (int it = blockIdx.x; it < items; it += gridDim.x) {
+      const int c = it / per_copy, in = it - c * per_copy;
+      const int lt = in / a.nh, head = in - lt * a.nh, layer = lt >> 1, t = lt & 1;
+      const int4 cp = list[c];
+      const int64_t from = (int64_t)cp.x * a.nh + head, to = (int64_t)cp.y * a.nh + head;
+      const int groups = cp.z >> 4;
+      auto move = [&](void* base, int unit) {   // 16-byte pieces of a head's filled rows
+        u4_t* p = reinterpret_cast<u4_t*>(base);
+        const int per_head = unit / 4, part = unit / 16 * groups;
+        for (int i = tid; i < part; i += 1024) {
+          u4_t v[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (i + 256 * k < part) v[k] = p[from * per_head + i + 256 * k];
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (i + 256 * k < part) p[to * per_head + i + 256 * k] = v[k];
+        }
+      };
+      move(a.data[layer][t], a.unit[0]);
+      if (a.unit[1] > 0) move(a.data[layer][2 + t], a.unit[1]);
+      if (a.unit[1] < 0 && tid == 0) {
+        float* f = reinterpret_cast<float*>(a.data[layer][2 + t]);
+        f[to] = f[from];
+      }
+    }
+    __syncthreads();   // the list has been read
   }
 }
 
@@ -582,6 +614,8 @@ extern "C" int fg_beam_reorder_paged(const fg_model_cfg* cfg, int32_t l, const f
   c.copies = a.copies;
   c.filled = a.filled;
   c.nh = cfg->nh;
+  c.rows = (int)rows;
+  if ((int64_t)1024 * kLayersPerLaunch * 2 * cfg->nh > 0x7fffffff) return FG_ERR_UNSUPPORTED;
   const int dh = cfg->h1 / cfg->nh, dt = pages[0].dtype;
   c.unit[0] = dt == FG_F16 ? 32 * dh : (dt == FG_I8P64 ? 16 * dh : 8 * dh);
   c.unit[1] = dt == FG_F16 ? 0 : (dt == FG_I8P64 ? -1 : 16 * (dh / kGroup) * (dt == FG_Q4G64 ? 8 : 4));
@@ -594,7 +628,9 @@ extern "C" int fg_beam_reorder_paged(const fg_model_cfg* cfg, int32_t l, const f
       c.data[j][2] = p.k_meta;
       c.data[j][3] = p.v_meta;
     }
-    hipLaunchKernelGGL(beam_copy_kernel, dim3((unsigned)rows, (unsigned)nl, c.unit[1] ? 4 : 2), dim3(256), 0, st, c);
+    c.layers = nl;
+    const int64_t most = rows * nl * 2 * cfg->nh;
+    hipLaunchKernelGGL(beam_copy_kernel, dim3((unsigned)(most < 2048 ? most : 2048)), dim3(256), 0, st, c);
     FG_LAUNCH_CHECK();
   }
   return FG_OK;
