@@ -561,14 +561,14 @@ def fg_beam_select(cfg: Cfg, logits: torch.Tensor, scores: torch.Tensor, beams: 
     assert rows % beams == 0
     n_best = beams if n_best is None else n_best
     n = rows // beams
-    ints = torch.empty((3, n, n_best), dtype=torch.int32, device=logits.device)
+    out_beams, ids, out_done = (torch.empty((n, n_best), dtype=torch.int32, device=logits.device) for _ in range(3))
     out = torch.empty((n, n_best), dtype=torch.float32, device=logits.device)
     if ws is None:
         ws = beam_select_workspace(cfg, n, beams, n_best)
     _check(lib().fg_beam_select(C.byref(cfg.c), n, beams, n_best, _p(logits), max(logits.stride(0), cfg.vocab), _p(scores),
-                                _p(done), eos, _p(ints[0]), _p(ints[1]), _p(out), _p(ints[2]), _p(ws), ws.numel(), _stream()),
+                                _p(done), eos, _p(out_beams), _p(ids), _p(out), _p(out_done), _p(ws), ws.numel(), _stream()),
            "fg_beam_select")
-    return ints[0], ints[1], out, ints[2]
+    return out_beams, ids, out, out_done
 
 
 def beam_reorder_workspace(n_groups: int, beams: int) -> torch.Tensor:

@@ -3,10 +3,10 @@
 //
 // Both products run on the integer matrix cores, on the stored codes as they are: no code is ever unpacked.  What stands on
 // the other side is a number in four digits of seven bits:
-//   q_d = (max |q| / C) * sum_t 2^(7t) a_td,   |a_td| <= 127,   C = 2^28 - 64     (signs in every digit)
-//   p_j =             1 / C  * sum_t 2^(7t) b_tj,  0 <= b_tj <= 127               (p = 2^(s - max over the page) <= 1)
-// so that q.k = (max|q| / C) S_k sum_t 2^(7t) (a_t . c) with exact 32-bit integer sums, put together in binary32.  Queries are
-// off by 2^-29 of their largest element, weights by 2^-28 of the page's largest: both below what binary32 sums lose.  The four
+//   q_d = (max |q| / Cq) * sum_t 2^(7t) a_td,   -64 <= a_td <= 63,   Cq = 133160000: +-Cq fit into such digits
+//   p_j =             1 / Cp * sum_t 2^(7t) b_tj,    0 <= b_tj <= 127,   Cp = 2^28 - 64     (p = 2^(s - max over the page) <= 1)
+// so that q.k = (max|q| / Cq) S_k sum_t 2^(7t) (a_t . c) with exact 32-bit integer sums, put together in binary32.  Queries are
+// off by 2^-26 of their largest element, weights by 2^-28 of the page's largest: below what binary32 sums lose.  The four
 // digits are four columns of v_mfma_i32_16x16x64_i8; its sixteen columns are four queries: the beams of a sequence that share
 // the page, or the query heads of a cache head, or (one query) idle, at no cost, because the loads are what bounds this.
 //
@@ -15,10 +15,10 @@
 //   O^T[d][column] += V^T . B^T   the lane group's 16 weights, packed to bytes, are the operand already; the pages hold the
 //                                 value codes of 16 positions next to each other, which is the other operand
 //
-// A unit is (group of rows, cache head, up to 4 NT queries); WPU waves share a unit's pages round-robin, and SPLITS workgroups
-// where the units are too few for the chip.  Each keeps a running (maximum, sum, output) per column; they are merged through
-// LDS, and through memory by a second launch where there are splits.  A wave has the values of a page and the keys of its next
-// one on their way while it computes.
+// A unit is (group of rows, cache head, four queries); the units of a cache head are neighbours, so that their waves find its
+// pages in the L1.  WPU waves share a unit's pages round-robin, and SPLITS workgroups where the units are too few for the chip.
+// Each keeps a running (maximum, sum, output) per column; they are merged through LDS, and through memory by a second launch
+// where there are splits.  A wave has the values of a page and the keys of its next one on their way while it computes.
 #include "fg_attn_common.h"
 
 namespace fg {
@@ -27,7 +27,9 @@ namespace {
 
 typedef int i4_t __attribute__((ext_vector_type(4)));
 
-constexpr float kDigits = 268435392.0f;   // C = 2^28 - 64: max|q| * (C / max|q|), off by two roundings, stays below 2^28
+constexpr float kWeightTop = 268435392.0f;
+constexpr float kQueryTop = 133160000.0f;                             // off by two roundings: 133160016 at most
+constexpr int kQueryShift = 64 * (1 + 128 + 16384 + 2097152);         // digits from 0: kQueryShift + 133160895 = 2^28 - 1
 
 struct AttnI8Args {
   const half_t* q;
@@ -53,10 +55,11 @@ __device__ __forceinline__ int seq_of(const AttnI8Args& a, int row) {
   const int sid = a.seq_ids ? a.seq_ids[row] : row;
   return sid < 0 ? 0 : (sid >= a.n_seqs ? a.n_seqs - 1 : sid);
 }
-__device__ __forceinline__ int rows_of(const AttnI8Args& a, int row) {
-  const int64_t n = (int64_t)a.seq_rows[row] + a.rows_bias, most = (int64_t)a.table_stride * FG_PAGE_ROWS;
+__device__ __forceinline__ int rows_in(const AttnI8Args& a, int cached) {
+  const int64_t n = (int64_t)cached + a.rows_bias, most = (int64_t)a.table_stride * FG_PAGE_ROWS;
   return (int)(n < 0 ? 0 : (n > most ? most : n));
 }
+__device__ __forceinline__ int rows_of(const AttnI8Args& a, int row) { return rows_in(a, a.seq_rows[row]); }
 // The same bits in the four lanes: each takes its own digit of what comes of it.  (A product that the compiler fused into the
 // first addition would be rounded in one lane and not in the other.)
 __device__ __forceinline__ float quad_sum(float v) {
@@ -65,14 +68,15 @@ __device__ __forceinline__ float quad_sum(float v) {
   return v + dpp_f32<kDppXor2>(v);
 }
 
-template <int DH, int NT, int WPU, bool SHARED>
-__global__ __launch_bounds__(256) void attn_decode_i8_kernel(AttnI8Args a) {
+template <int DH, int WPU, bool SHARED>
+__global__ __launch_bounds__(256, 3) void attn_decode_i8_kernel(AttnI8Args a) {
   constexpr int KS = DH / 64;   // steps of 64 over the head size
   constexpr int ND = DH / 16;   // blocks of 16 output rows
   constexpr int UPB = 4 / WPU;  // units per workgroup
-  extern __shared__ uint2 sm_list[];   // SHARED: [wave][64 * beams] pages to visit: {page, slot in the window | beams << 8}
+  // SHARED: the wave's pages to visit, 64 a beam at most: {page, slot in the window | beams << 8}
+  __shared__ uint2 sm_list[SHARED ? 4 : 1][SHARED ? 5 * 64 : 1];
   __shared__ float sm_m[4][4], sm_l[4][4];
-  __shared__ float sm_o[4][4][DH];
+  __shared__ __attribute__((aligned(16))) float sm_o[4][4][DH];
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -83,21 +87,17 @@ __global__ __launch_bounds__(256) void attn_decode_i8_kernel(AttnI8Args a) {
   const int chunk = unit % a.chunks, gh = unit / a.chunks;
   const int kv = gh % a.nkv, group = gh / a.nkv;
   const int col = lane & 15, g = lane >> 4, dig = col & 3;
-  const int per_kv = a.nh / a.nkv, nq = per_kv * a.beams, q_lo = chunk * 4 * NT;
+  const int per_kv = a.nh / a.nkv, nq = per_kv * a.beams;
   const int split = blockIdx.y;
 
-  // ---- the lane's query of every tile: its digits, its number of rows
-  i4_t qop[NT][KS];
-  float qmul[NT];
-  int n_of[NT], beam_of[NT];
-  int n_max = 0;
-#pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    const int qi = q_lo + 4 * t + (col >> 2);
-    const bool valid = qi < nq;
-    const int qc = valid ? qi : nq - 1;
-    const int beam = qc / per_kv, row = group * a.beams + beam;
-    const half_t* src = a.q + (int64_t)row * a.q_stride + (int64_t)(kv * per_kv + qc % per_kv) * DH + 16 * g;
+  // ---- the lane's query: its digit of every element, its number of rows
+  const int qi = 4 * chunk + (col >> 2), qc = min(qi, nq - 1);
+  const int beam = qc / per_kv, row = group * a.beams + beam, head = kv * per_kv + qc - beam * per_kv;
+  const int n_row = rows_of(a, row);
+  i4_t qop[KS];
+  float qmul;
+  {
+    const half_t* src = a.q + (int64_t)row * a.q_stride + (int64_t)head * DH + 16 * g;
     h8_t x[KS][2];
     float top = 0.f;
 #pragma unroll
@@ -109,40 +109,30 @@ __global__ __launch_bounds__(256) void attn_decode_i8_kernel(AttnI8Args a) {
         for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf((float)x[k][h][e]));
       }
     top = xor32_reduce(xor16_reduce(top, OpMax()), OpMax());
-    const float inv = top > 0.f ? kDigits / top : 0.f;
+    const float inv = top > 0.f ? kQueryTop / top : 0.f;
 #pragma unroll
     for (int k = 0; k < KS; ++k)
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
-        uint32_t word = 0;
+        uint32_t d[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float f = (float)x[k][w >> 1][4 * (w & 1) + e] * inv;
-          const int mag = (((int)rintf(fabsf(f)) >> (7 * dig)) & 127);
-          word |= (uint32_t)((f < 0.f ? -mag : mag) & 255) << (8 * e);
-        }
-        qop[t][k][w] = (int)word;
+        for (int e = 0; e < 4; ++e)
+          d[e] = ((uint32_t)((int)((float)x[k][w >> 1][4 * (w & 1) + e] * inv) + kQueryShift) >> (7 * dig)) & 127u;
+        const uint32_t y = (d[0] | d[1] << 8 | d[2] << 16 | d[3] << 24) ^ 0x40404040u;   // less 64, in eight bits
+        qop[k][w] = (int)(y | (y & 0x40404040u) << 1);
       }
     // scores come out in log2 units; the digit's weight goes in here
-    qmul[t] = top * (a.scale * kLog2e / kDigits) * (float)(1 << (7 * dig));
-    const int n = rows_of(a, row);
-    n_of[t] = valid ? n : 0x7fffffff;   // an idle column is never masked, and never written
-    beam_of[t] = beam;
-    n_max = max(n_max, n);
+    qmul = top * (a.scale * kLog2e / kQueryTop) * (float)(1 << (7 * dig));
   }
-  n_max = __builtin_amdgcn_readfirstlane((int)wave_max((float)((n_max + 63) >> 6)));   // pages: exact in binary32
+  const int n_of = qi < nq ? n_row : 0x7fffffff;   // an idle column is never masked, and never written
+  const int n_max = __builtin_amdgcn_readfirstlane((int)wave_max((float)((n_row + 63) >> 6)));   // pages: exact in binary32
   const int per_split = (n_max + a.splits - 1) / a.splits;
   const int s_lo = split * per_split, s_hi = min(n_max, s_lo + per_split);
 
-  float m_run[NT], l_run[NT];
-  f4_t o[NT][ND];
+  float m_run = -INFINITY, l_run = 0.f;
+  f4_t o[ND];
 #pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    m_run[t] = -INFINITY;
-    l_run[t] = 0.f;
-#pragma unroll
-    for (int j = 0; j < ND; ++j) o[t][j] = (f4_t){0.f, 0.f, 0.f, 0.f};
-  }
+  for (int j = 0; j < ND; ++j) o[j] = (f4_t){0.f, 0.f, 0.f, 0.f};
 
   i4_t kreg[4][KS], vreg[ND];
   const int64_t page_bytes = FG_PAGE_ROWS * DH;
@@ -160,205 +150,189 @@ __global__ __launch_bounds__(256) void attn_decode_i8_kernel(AttnI8Args a) {
     for (int j = 0; j < ND; ++j) vreg[j] = *reinterpret_cast<const i4_t*>(p + 256 * j);
   };
 
-  const int b_lo = q_lo / per_kv, b_hi = min(nq - 1, q_lo + 4 * NT - 1) / per_kv;   // beams of this unit
+  const int b_lo = 4 * chunk / per_kv, nb = min(nq - 1, 4 * chunk + 3) / per_kv - b_lo + 1;   // beams of this unit
   const int32_t* tbl0 = a.page_table + (int64_t)seq_of(a, group * a.beams + b_lo) * a.table_stride;
-  uint2* list = sm_list + wave * 64 * a.beams;
   auto clamp_page = [&](int pg) { return pg < 0 ? 0 : (pg >= a.n_pages ? a.n_pages - 1 : pg); };
 
   for (int w0 = s_lo + part; w0 < s_hi; w0 += 64 * WPU) {   // windows of 64 of this wave's slots
     const int slot_l = w0 + WPU * lane;
     const bool in = slot_l < s_hi;
-    int count, pages = 0;
+    int count = 0;
+    uint32_t e_page = 0, e_info = 0;   // 64 pages to visit, one per lane; SHARED: slot in the window | beams << 8
+    uint2* list = sm_list[SHARED ? wave : 0];
     if constexpr (SHARED) {
       // every page once, with the beams that name it; in the order of the beams, then of the slots
-      int e[FG_MAX_BEAMS];
+      const int slot_c = in ? slot_l : w0;
+      int e[4], n_k[4];
 #pragma unroll
-      for (int k = 0; k < FG_MAX_BEAMS; ++k) {
-        e[k] = -1;
-        if (k <= b_hi - b_lo) {
-          const int row = group * a.beams + b_lo + k;
-          if (in && rows_of(a, row) > (slot_l << 6))
-            e[k] = clamp_page(a.page_table[(int64_t)seq_of(a, row) * a.table_stride + slot_l]);
-        }
+      for (int k = 0; k < 4; ++k) {   // all loads first (beams that are not there: the last one's again)
+        const int r = group * a.beams + b_lo + min(k, nb - 1);
+        n_k[k] = a.seq_rows[r];
+        e[k] = a.page_table[(int64_t)seq_of(a, r) * a.table_stride + slot_c];
       }
-      count = 0;
 #pragma unroll
-      for (int k = 0; k < FG_MAX_BEAMS; ++k) {
-        if (k > b_hi - b_lo) break;
+      for (int k = 0; k < 4; ++k) e[k] = in && k < nb && rows_in(a, n_k[k]) > (slot_l << 6) ? clamp_page(e[k]) : -1 - k;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
         bool first = e[k] >= 0;
-#pragma unroll
-        for (int i = 0; i < k; ++i) first = first && e[i] != e[k];
         uint32_t who = 0;
 #pragma unroll
-        for (int i = k; i < FG_MAX_BEAMS; ++i) who |= e[i] == e[k] ? 1u << i : 0u;
+        for (int i = 0; i < 4; ++i) {
+          if (i < k) first = first && e[i] != e[k];
+          if (i >= k) who |= e[i] == e[k] ? 1u << i : 0u;
+        }
         const uint64_t m = __builtin_amdgcn_ballot_w64(first);
         const int at = count + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0u));
         if (first) list[at] = make_uint2((uint32_t)e[k], (uint32_t)lane | who << 8);
         count += __builtin_popcountll(m);
       }
       wave_lds_fence();
+      const uint2 mine = list[lane];   // (what lies behind the last entry is not asked for)
+      e_page = mine.x, e_info = mine.y;
     } else {
       count = __builtin_popcountll(__builtin_amdgcn_ballot_w64(in));
-      pages = clamp_page(tbl0[in ? slot_l : w0]);
+      e_page = (uint32_t)clamp_page(tbl0[in ? slot_l : w0]);
     }
-    auto visit = [&](int v, int& page, int& slot, uint32_t& who) {
-      if constexpr (SHARED) {
-        const uint2 e = list[v];
-        page = __builtin_amdgcn_readfirstlane(e.x);
-        const uint32_t y = __builtin_amdgcn_readfirstlane(e.y);
-        slot = w0 + WPU * (int)(y & 255);
-        who = y >> 8;
-      } else {
-        page = __builtin_amdgcn_readlane(pages, v);
-        slot = w0 + WPU * v;
-        who = 1;
-      }
-    };
+    auto slot_at = [&](uint32_t info, int v) { return w0 + WPU * (SHARED ? (int)(info & 255) : v); };
 
     int page = 0, slot = 0;
     uint32_t who = 0;
     if (count > 0) {
-      visit(0, page, slot, who);
+      page = __builtin_amdgcn_readfirstlane(e_page);
+      who = __builtin_amdgcn_readfirstlane(e_info);
+      slot = slot_at(who, 0);
       load_k(page);
     }
     for (int v = 0; v < count; ++v) {
       const float ks = a.k_scales[(int64_t)page * a.nkv + kv], vs = a.v_scales[(int64_t)page * a.nkv + kv];
       load_v(page);
-      int page_n = page, slot_n = slot;
-      uint32_t who_n = who;
-      if (v + 1 < count) visit(v + 1, page_n, slot_n, who_n);
+      if (SHARED && ((v + 1) & 63) == 0) {
+        const uint2 next = list[v + 1 + lane];
+        e_page = next.x, e_info = next.y;
+      }
+      const int page_n = __builtin_amdgcn_readlane(e_page, (v + 1) & 63);
+      const uint32_t who_n = __builtin_amdgcn_readlane(e_info, (v + 1) & 63);
       __builtin_amdgcn_sched_barrier(0);
-      i4_t acc[NT][4];
+      i4_t acc[4];
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
+      for (int i = 0; i < 4; ++i) {
+        acc[i] = (i4_t){0, 0, 0, 0};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          acc[t][i] = (i4_t){0, 0, 0, 0};
-#pragma unroll
-          for (int k = 0; k < KS; ++k)
-            acc[t][i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(kreg[i][k], qop[t][k], acc[t][i], 0, 0, 0);
-        }
+        for (int k = 0; k < KS; ++k) acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(kreg[i][k], qop[k], acc[i], 0, 0, 0);
+      }
       __builtin_amdgcn_sched_barrier(0);
       if (v + 1 < count) load_k(page_n);
       __builtin_amdgcn_sched_barrier(0);
+      const float f = qmul * ks;
+      float s[4][4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s[i][r] = quad_sum((float)acc[i][r] * f);
       const int left = slot << 6;
-#pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        const float f = qmul[t] * ks;
-        float s[4][4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) s[i][r] = quad_sum((float)acc[t][i][r] * f);
-        const bool mine = !SHARED || (who >> (beam_of[t] - b_lo) & 1) || n_of[t] == 0x7fffffff;
-        if (__builtin_amdgcn_ballot_w64(!mine || left > n_of[t] - 64) != 0) {
-          const int n = mine ? n_of[t] - left - 16 * g : 0;   // keys of the lane's sixteen that count
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) s[i][r] = 4 * i + r < n ? s[i][r] : -INFINITY;
-        }
-        float top = -INFINITY;
+      const bool mine = !SHARED || (who >> (8 + beam - b_lo) & 1) || n_of == 0x7fffffff;
+      if (__builtin_amdgcn_ballot_w64(!mine || left > n_of - 64) != 0) {
+        const int n = mine ? n_of - left - 16 * g : 0;   // keys of the lane's sixteen that count
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) top = fmaxf(top, s[i][r]);
-        top = xor32_reduce(xor16_reduce(top, OpMax()), OpMax());
-        const float use = top == -INFINITY ? 0.f : top;
-        const float m_new = fmaxf(m_run[t], top), m_use = m_new == -INFINITY ? 0.f : m_new;
-        const float alpha = fast_exp2(m_run[t] - m_use), beta = fast_exp2(top - m_use);
-        m_run[t] = m_new;
-        float sum = 0.f;
-        i4_t pop;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          uint32_t d[4];
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const float p = fast_exp2(s[i][r] - use);
-            sum += p;
-            d[r] = ((uint32_t)(p * kDigits) >> (7 * dig)) & 127u;
-          }
-          pop[i] = (int)(d[0] | d[1] << 8 | d[2] << 16 | d[3] << 24);
-        }
-        l_run[t] = l_run[t] * alpha + sum * beta;
-        if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
-#pragma unroll
-          for (int j = 0; j < ND; ++j) o[t][j] *= alpha;
-        }
-        const float bv = beta * vs;
-#pragma unroll
-        for (int j = 0; j < ND; ++j) {
-          const i4_t z = {0, 0, 0, 0};
-          const i4_t po = __builtin_amdgcn_mfma_i32_16x16x64_i8(vreg[j], pop, z, 0, 0, 0);
-#pragma unroll
-          for (int r = 0; r < 4; ++r) o[t][j][r] = __builtin_fmaf((float)po[r], bv, o[t][j][r]);
-        }
+          for (int r = 0; r < 4; ++r) s[i][r] = 4 * i + r < n ? s[i][r] : -INFINITY;
       }
-      page = page_n, slot = slot_n, who = who_n;
+      float top = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) top = fmaxf(top, s[i][r]);
+      top = xor32_reduce(xor16_reduce(top, OpMax()), OpMax());
+      const float use = top == -INFINITY ? 0.f : top;
+      const float m_new = fmaxf(m_run, top), m_use = m_new == -INFINITY ? 0.f : m_new;
+      const float alpha = fast_exp2(m_run - m_use), beta = fast_exp2(top - m_use);
+      m_run = m_new;
+      float sum = 0.f;
+      i4_t pop;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint32_t d[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float p = fast_exp2(s[i][r] - use);
+          sum += p;
+          d[r] = ((uint32_t)(p * kWeightTop) >> (7 * dig)) & 127u;
+        }
+        pop[i] = (int)(d[0] | d[1] << 8 | d[2] << 16 | d[3] << 24);
+      }
+      l_run = l_run * alpha + sum * beta;
+      if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
+#pragma unroll
+        for (int j = 0; j < ND; ++j) o[j] *= alpha;
+      }
+      const float bv = beta * vs;
+#pragma unroll
+      for (int j = 0; j < ND; ++j) {
+        const i4_t z = {0, 0, 0, 0};
+        const i4_t po = __builtin_amdgcn_mfma_i32_16x16x64_i8(vreg[j], pop, z, 0, 0, 0);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) o[j][r] = __builtin_fmaf((float)po[r], bv, o[j][r]);
+      }
+      page = page_n, who = who_n, slot = slot_at(who_n, v + 1);
     }
     if constexpr (SHARED) wave_lds_fence();   // the list is read before it is written again
   }
 
   // ---- digits together, then waves, then (second launch) splits
-  const float wd = (float)(1 << (7 * dig)) / kDigits;
+  const float wd = (float)(1 << (7 * dig)) / kWeightTop;
+  const float l = xor32_reduce(xor16_reduce(l_run, OpAdd()), OpAdd());
 #pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    const float l = xor32_reduce(xor16_reduce(l_run[t], OpAdd()), OpAdd());
-    f4_t x[ND];
+  for (int j = 0; j < ND; ++j)
 #pragma unroll
-    for (int j = 0; j < ND; ++j)
+    for (int r = 0; r < 4; ++r) o[j][r] = quad_sum(o[j][r] * wd);
+  if (WPU == 1 && a.splits == 1) {
+    if (qi < nq && there) {
+      const float inv = l > 0.f ? 1.0f / l : 0.f;   // no rows attended: zeros
+      half_t* dst = a.out + ((int64_t)row * a.nh + head) * DH + 4 * g;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) x[j][r] = quad_sum(o[t][j][r] * wd);
-    const int qi = q_lo + 4 * t + (col >> 2);
-    if (WPU == 1 && a.splits == 1) {
-      if (qi < nq && there) {
-        const int row = group * a.beams + qi / per_kv, head = kv * per_kv + qi % per_kv;
-        const float inv = l > 0.f ? 1.0f / l : 0.f;   // no rows attended: zeros
-        half_t* dst = a.out + ((int64_t)row * a.nh + head) * DH + 4 * g;
+      for (int j = 0; j < ND; ++j)
+        if ((j & 3) == dig) {
+          h4_t h;
 #pragma unroll
-        for (int j = 0; j < ND; ++j)
-          if ((j & 3) == dig) {
-            h4_t h;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) h[r] = (half_t)(x[j][r] * inv);
-            *reinterpret_cast<h4_t*>(dst + 16 * j) = h;
-          }
-      }
-      continue;
+          for (int r = 0; r < 4; ++r) h[r] = (half_t)(o[j][r] * inv);
+          *reinterpret_cast<h4_t*>(dst + 16 * j) = h;
+        }
     }
-    if (t > 0) __syncthreads();   // the tile before has been read
-    if (lane < 16 && dig == 0) {
-      sm_m[wave][col >> 2] = m_run[t];
-      sm_l[wave][col >> 2] = l;
+    return;
+  }
+  if (lane < 16 && dig == 0) {
+    sm_m[wave][col >> 2] = m_run;
+    sm_l[wave][col >> 2] = l;
+  }
+#pragma unroll
+  for (int j = 0; j < ND; ++j)
+    if ((j & 3) == dig) *reinterpret_cast<f4_t*>(&sm_o[wave][col >> 2][16 * j + 4 * g]) = o[j];
+  __syncthreads();
+  for (int i = wave; i < UPB * 4; i += 4) {   // a wave per query
+    const int qs = i & 3, u = i >> 2, un = unit0 + u;
+    const int qn = un % a.chunks * 4 + qs;
+    if (un >= a.n_units || qn >= nq) continue;
+    const int gn = un / a.chunks, bn = qn / per_kv;
+    const int64_t rh = (int64_t)(gn / a.nkv * a.beams + bn) * a.nh + gn % a.nkv * per_kv + qn - bn * per_kv;
+    float M = -INFINITY, den = 0.f, num[KS] = {};
+#pragma unroll
+    for (int w = 0; w < WPU; ++w) M = fmaxf(M, sm_m[u * WPU + w][qs]);
+#pragma unroll
+    for (int w = 0; w < WPU; ++w) {
+      const float mw = sm_m[u * WPU + w][qs], fw = mw == -INFINITY ? 0.f : fast_exp2(mw - M);
+      den += fw * sm_l[u * WPU + w][qs];
+#pragma unroll
+      for (int k = 0; k < KS; ++k) num[k] += fw * sm_o[u * WPU + w][qs][lane + 64 * k];
     }
 #pragma unroll
-    for (int j = 0; j < ND; ++j)
-      if ((j & 3) == dig) *reinterpret_cast<f4_t*>(&sm_o[wave][col >> 2][16 * j + 4 * g]) = x[j];
-    __syncthreads();
-    for (int i = tid; i < UPB * 4 * DH; i += 256) {
-      const int d = i % DH, qs = i / DH % 4, u = i / (4 * DH);
-      const int un = unit0 + u;
-      const int qn = un % a.chunks * 4 * NT + 4 * t + qs;
-      if (un >= a.n_units || qn >= nq) continue;
-      const int row = un / a.chunks / a.nkv * a.beams + qn / per_kv, head = un / a.chunks % a.nkv * per_kv + qn % per_kv;
-      float M = -INFINITY, num = 0.f, den = 0.f;
-#pragma unroll
-      for (int w = 0; w < WPU; ++w) M = fmaxf(M, sm_m[u * WPU + w][qs]);
-#pragma unroll
-      for (int w = 0; w < WPU; ++w) {
-        const float mw = sm_m[u * WPU + w][qs], fw = mw == -INFINITY ? 0.f : fast_exp2(mw - M);
-        num += fw * sm_o[u * WPU + w][qs][d];
-        den += fw * sm_l[u * WPU + w][qs];
-      }
-      const int64_t rh = (int64_t)row * a.nh + head;
-      if (a.splits == 1) {
-        a.out[rh * DH + d] = (half_t)(den > 0.f ? num / den : 0.f);
-      } else {
-        a.part_o[(rh * a.splits + split) * DH + d] = num;
-        if (d == 0) a.part_ml[rh * a.splits + split] = make_float2(M, den);
-      }
+    for (int k = 0; k < KS; ++k) {
+      if (a.splits == 1)
+        a.out[rh * DH + lane + 64 * k] = (half_t)(den > 0.f ? num[k] / den : 0.f);
+      else
+        a.part_o[(rh * a.splits + split) * DH + lane + 64 * k] = num[k];
     }
+    if (a.splits > 1 && lane == 0) a.part_ml[rh * a.splits + split] = make_float2(M, den);
   }
 }
 
@@ -396,22 +370,36 @@ __global__ __launch_bounds__(256) void attn_merge_i8_kernel(AttnI8Args a) {
 }
 
 struct Plan {
-  int nt, chunks, wpu, splits;
+  int chunks, wpu, splits;
   int64_t units;
 };
 size_t part_bytes(int64_t rows_heads, int splits, int dh) { return splits > 1 ? align_up((size_t)rows_heads * splits * (dh + 2) * 4, 256) : 0; }
 
+// Waves per unit, and workgroups that share a sequence.  Only the device knows the lengths; what the table could hold stands for
+// them.  Measured, us with 1 / 2 / 4 waves a unit, pages of 64 rows at head size 128:
+//   6144 units, 2 pages 39 / 43 / 54         2048 units, 2 pages 14.4 / 17.6 / 19.5, 7 pages 42.7 / 44.0 / 44.8,
+//   2048 units of 1 to 32 pages (table of 32) 115 / 107 / 104       1536 units of four beams, 8 shared pages 60.9 / 58.3 / 59.6
+//   768 units of four beams, head size 64, 9 pages 19.2 / 18.4 / 18.0    128 units, 32 pages 39.5 / 23.3 / 15.0
+//   1024 units, four to a cache head (their waves meet in the L1 if they share a workgroup) 46.8 / 50.8 / 81.2
+// and where units are few, with 1 / 2 / 4 / 8 / 16 / 32 splits of four waves:
+//   128 units, 32 pages 15.0 / 17.0 / 16.7 / 19.2    32 units, 24 pages 17.1 / 16.4 / 15.4 / 14.6, 125 pages 39.6 / 25.4 / 17.7 / 16.8 /
+//   16.5 / 19.0    8 units, 512 pages 144 / 77 / 43 / 26 / 17.7 / 17.4
 Plan plan_i8(int32_t nh, int32_t nkv, int32_t beams, int32_t b, int32_t table_stride) {
   Plan p;
-  const int nq = nh / nkv * beams;
-  p.nt = nq <= 4 ? 1 : (nq <= 8 ? 2 : 4);
-  p.chunks = (int)ceil_div(nq, 4 * p.nt);
+  p.chunks = (int)ceil_div(nh / nkv * beams, 4);
   p.units = (int64_t)(b / beams) * nkv * p.chunks;
-  p.wpu = p.units >= 2048 ? 1 : (p.units >= 1024 ? 2 : 4);
-  const int64_t want = ceil_div(1024, p.units), most = ceil_div(table_stride, 8);   // two pages a wave at least
-  p.splits = p.wpu < 4 ? 1 : (int)(want < most ? want : most);
-  if (p.splits > kMostSplits) p.splits = kMostSplits;
-  if (p.splits < 1) p.splits = 1;
+  if (p.units < 1024)
+    p.wpu = 4;
+  else if (p.chunks >= 4 || (p.units >= 2048 && table_stride < 16))
+    p.wpu = 1;
+  else
+    p.wpu = 2;
+  p.splits = 1;
+  if (p.units <= 64 && table_stride >= 24) {   // two pages a wave at least
+    const int64_t want = 512 / p.units, most = table_stride / 8;
+    p.splits = (int)(want < most ? want : most);
+    if (p.splits > kMostSplits) p.splits = kMostSplits;
+  }
   return p;
 }
 
@@ -456,26 +444,22 @@ int decode_attention_i8_launch(const fg_model_cfg& cfg, int32_t nkv, int32_t bea
   a.part_o = reinterpret_cast<float*>(ws);
   a.part_ml = reinterpret_cast<float2*>(a.part_o + (p.splits > 1 ? rh * p.splits * dh : 0));
   const dim3 grid((unsigned)ceil_div(p.units * p.wpu, 4), (unsigned)p.splits);
-  const size_t lds = beams > 1 ? (size_t)4 * 64 * beams * sizeof(uint2) : 0;
+  const bool shared = beams > 1 && cfg.nh / nkv % 4 != 0;   // else a unit has queries of one row only
   ProfScope prof(FG_K_ATTN_DECODE, stream);
-#define FG_I8(DH_, NT_, WPU_, SH_) hipLaunchKernelGGL((attn_decode_i8_kernel<DH_, NT_, WPU_, SH_>), grid, dim3(256), lds, stream, a)
-#define FG_I8_SH(DH_, NT_, WPU_)                                                     \
-  do {                                                                               \
-    if (beams > 1) FG_I8(DH_, NT_, WPU_, true); else FG_I8(DH_, NT_, WPU_, false);   \
+#define FG_I8_SH(DH_, WPU_)                                                                              \
+  do {                                                                                                   \
+    if (shared)                                                                                          \
+      hipLaunchKernelGGL((attn_decode_i8_kernel<DH_, WPU_, true>), grid, dim3(256), 0, stream, a);       \
+    else                                                                                                 \
+      hipLaunchKernelGGL((attn_decode_i8_kernel<DH_, WPU_, false>), grid, dim3(256), 0, stream, a);      \
   } while (0)
-#define FG_I8_WPU(DH_, NT_)                                                                                       \
-  do {                                                                                                            \
-    if (p.wpu == 1) FG_I8_SH(DH_, NT_, 1); else if (p.wpu == 2) FG_I8_SH(DH_, NT_, 2); else FG_I8_SH(DH_, NT_, 4); \
+#define FG_I8(DH_)                                                                                              \
+  do {                                                                                                          \
+    if (p.wpu == 1) FG_I8_SH(DH_, 1); else if (p.wpu == 2) FG_I8_SH(DH_, 2); else FG_I8_SH(DH_, 4);              \
   } while (0)
-#define FG_I8_NT(DH_)                                                                                  \
-  do {                                                                                                 \
-    if (p.nt == 1) FG_I8_WPU(DH_, 1); else if (p.nt == 2) FG_I8_WPU(DH_, 2); else FG_I8_WPU(DH_, 4);   \
-  } while (0)
-  if (dh == 128) FG_I8_NT(128); else FG_I8_NT(64);
-#undef FG_I8_NT
-#undef FG_I8_WPU
-#undef FG_I8_SH
+  if (dh == 128) FG_I8(128); else FG_I8(64);
 #undef FG_I8
+#undef FG_I8_SH
   FG_LAUNCH_CHECK();
   if (p.splits > 1) {
     if (dh == 128)
