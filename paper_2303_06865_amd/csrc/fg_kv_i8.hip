@@ -34,7 +34,7 @@ struct AppendI8Args {
   int8_t* codes[2];
   float* scales[2];
   int64_t ld;
-  int32_t b, s, nh, slots, head_groups;   // slots: pages that the s rows of a sequence can touch; head_groups: workgroups a row of heads takes
+  int32_t b, s, nh, slots;   // slots: pages that the s rows of a sequence can touch
   PageRows at;
 };
 
@@ -89,91 +89,98 @@ __device__ __forceinline__ int unit_at(int group, int d) {
   return (group * DH + (d & ~7) + (((d & 7) + (d >> 3)) & 7)) * 16;
 }
 
-// One wave per (sequence of the call, page it touches, head, K or V), in four groups of 16 positions; lane = 8 head dimensions
-// (lane % LR) of RPL positions of each group.  The page's new rows stay in registers until their largest magnitude is known.
-// Value codes pass through LDS and leave in their units, in order (straight from the lanes, 16 bytes in every 128, storing
-// 16 x 500 rows of 32 heads took 70 us).
+// One workgroup per (sequence of the call, page it touches, head, K or V), a wave per group of 16 positions; lane = 8 head dimensions
+// (lane % LR) of RPL positions.  The new rows stay in registers until the page's largest magnitude is known.  Value codes pass
+// through LDS and leave in their units, in order.  Storing 16 x 500 rows of 32 heads: with units straight from the lanes, 16
+// bytes in every 128, 70 us; in order, a wave per page 54; this 52, 3.8 TB/s of rows read and codes written.
 template <int DH, bool VALUES>
 __device__ __forceinline__ void store_rows(const half_t* src, int64_t ld, int8_t* codes, float* scale, int lo, int hi, int lane,
-                                           uint8_t* sm) {
-  constexpr int LR = DH / 8, RPL = LR / 4, UPL = DH / 64;   // positions of a group, units of a group per lane
-  __asm__ volatile("" : "+v"(lane));   // addresses are made here, not kept in registers from before the caller's loop
-  const int d0 = (lane % LR) * 8, r0 = (lane / LR) * RPL;
+                                           int q, uint8_t* sm, float* sm_top) {
+  constexpr int LR = DH / 8, RPL = LR / 4, UPL = DH / 64;   // positions, units per lane
+  const int d0 = (lane % LR) * 8, r0 = 16 * q + (lane / LR) * RPL;
+  const bool touched = 16 * q < hi && 16 * q + 16 > lo;
   const float was = lo > 0 ? *scale : 0.f;
-  h8_t x[4][RPL];
-#pragma unroll
-  for (int q = 0; q < 4; ++q)
+  h8_t x[RPL];
+  us8_t top = (us8_t)(uint16_t)0;
+  if (touched) {
 #pragma unroll
     for (int n = 0; n < RPL; ++n) {
-      int row = 16 * q + r0 + n;
+      int row = r0 + n;
       row = row < lo ? lo : (row < hi ? row : hi - 1);   // a new row again in the place of one that is not: the largest stays
-      x[q][n] = *reinterpret_cast<const h8_t*>(src + (int64_t)(row - lo) * ld + d0);
+      x[n] = *reinterpret_cast<const h8_t*>(src + (int64_t)(row - lo) * ld + d0);
     }
-  us8_t top = (us8_t)(uint16_t)0;
 #pragma unroll
-  for (int q = 0; q < 4; ++q)
+    for (int n = 0; n < RPL; ++n) top = abs_max(x[n], top);
+  }
+  const float wt = wave_max(largest(top));
+  if (lane == 0) sm_top[q] = wt;
+  __syncthreads();
+  const Step st = step_of(fmaxf(fmaxf(sm_top[0], sm_top[1]), fmaxf(sm_top[2], sm_top[3])), was, lo > 0);   // the same in all lanes
+  if (q == 0 && lane == 0) *scale = st.now;
+  if (!touched) {   // x holds nothing: only old codes, if any
+    if (st.grown)
 #pragma unroll
-    for (int n = 0; n < RPL; ++n) top = abs_max(x[q][n], top);
-  const Step st = step_of(wave_max(largest(top)), was, lo > 0);   // the same in all lanes
-#pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    __builtin_amdgcn_sched_barrier(0);   // one group's codes at a time in registers
-    if (!(st.grown || (16 * q < hi && 16 * q + 16 > lo))) continue;
-    if constexpr (!VALUES) {
-#pragma unroll
-      for (int n = 0; n < RPL; ++n) {
-        const int row = 16 * q + r0 + n;
-        u2_t* dst = reinterpret_cast<u2_t*>(codes + row * DH + d0);
-        if (row >= lo && row < hi)
-          *dst = row_codes(x[q][n], st);
-        else if (st.grown)
-          *dst = codes_again(*dst, st);
-      }
-    } else {
-      wave_lds_fence();   // what was read from there before has been
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        uint8_t* to = sm + unit_at<DH>(0, d0 + e) + r0;
-        const uint32_t c0 = code_of(x[q][0][e], st), c1 = code_of(x[q][1][e], st);
-        if constexpr (RPL == 4)
-          *reinterpret_cast<uint32_t*>(to) = bytes4(c0, c1, code_of(x[q][2][e], st), code_of(x[q][3][e], st));
-        else
-          *reinterpret_cast<uint16_t*>(to) = (uint16_t)__builtin_amdgcn_perm(c1, c0, 0x0c0c0400u);
-      }
-      wave_lds_fence();
-      const bool whole = 16 * q >= lo && 16 * q + 16 <= hi;
-#pragma unroll
-      for (int t = 0; t < UPL; ++t) {
+      for (int t = 0; t < UPL; ++t) {   // (16 rows of keys are as many bytes)
         u4_t* dst = reinterpret_cast<u4_t*>(codes + (q * DH + 64 * t + lane) * 16);
-        u4_t c = *reinterpret_cast<const u4_t*>(sm + unit_at<DH>(0, 64 * t + lane));
-        if (!whole) {   // the unit's other positions stay, in the page's new step
-          const u4_t old = *dst;
-#pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            uint32_t m = 0;
-#pragma unroll
-            for (int n = 0; n < 4; ++n) {
-              const int row = 16 * q + 4 * w + n;
-              const int8_t o = (int8_t)(old[w] >> (8 * n));
-              const uint32_t v = row >= lo && row < hi ? c[w] >> (8 * n) : (st.grown ? again(o, st) : (uint32_t)o);
-              m |= (v & 255u) << (8 * n);
-            }
-            c[w] = m;
-          }
-        }
-        *dst = c;
+        u4_t c = *dst;
+        const u2_t a = codes_again((u2_t){c.x, c.y}, st), b = codes_again((u2_t){c.z, c.w}, st);
+        *dst = (u4_t){a.x, a.y, b.x, b.y};
       }
+    return;
+  }
+  if constexpr (!VALUES) {
+#pragma unroll
+    for (int n = 0; n < RPL; ++n) {
+      const int row = r0 + n;
+      u2_t* dst = reinterpret_cast<u2_t*>(codes + row * DH + d0);
+      if (row >= lo && row < hi)
+        *dst = row_codes(x[n], st);
+      else if (st.grown)
+        *dst = codes_again(*dst, st);
+    }
+  } else {
+    wave_lds_fence();   // what was read from there before has been
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      uint8_t* to = sm + unit_at<DH>(0, d0 + e) + (lane / LR) * RPL;
+      const uint32_t c0 = code_of(x[0][e], st), c1 = code_of(x[1][e], st);
+      if constexpr (RPL == 4)
+        *reinterpret_cast<uint32_t*>(to) = bytes4(c0, c1, code_of(x[2][e], st), code_of(x[3][e], st));
+      else
+        *reinterpret_cast<uint16_t*>(to) = (uint16_t)__builtin_amdgcn_perm(c1, c0, 0x0c0c0400u);
+    }
+    wave_lds_fence();
+    const bool whole = 16 * q >= lo && 16 * q + 16 <= hi;
+#pragma unroll
+    for (int t = 0; t < UPL; ++t) {
+      u4_t* dst = reinterpret_cast<u4_t*>(codes + (q * DH + 64 * t + lane) * 16);
+      u4_t c = *reinterpret_cast<const u4_t*>(sm + unit_at<DH>(0, 64 * t + lane));
+      if (!whole) {   // the unit's other positions stay, in the page's new step
+        const u4_t old = *dst;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          uint32_t m = 0;
+#pragma unroll
+          for (int n = 0; n < 4; ++n) {
+            const int row = 16 * q + 4 * w + n;
+            const int8_t o = (int8_t)(old[w] >> (8 * n));
+            const uint32_t v = row >= lo && row < hi ? c[w] >> (8 * n) : (st.grown ? again(o, st) : (uint32_t)o);
+            m |= (v & 255u) << (8 * n);
+          }
+          c[w] = m;
+        }
+      }
+      *dst = c;
     }
   }
-  if (lane == 0) *scale = st.now;
 }
 
 template <int DH>
-__global__ __launch_bounds__(256, 4) void kv_append_i8_kernel(AppendI8Args a) {
+__global__ __launch_bounds__(256) void kv_append_i8_kernel(AppendI8Args a) {
   __shared__ __attribute__((aligned(16))) uint8_t sm[4][16 * DH];
+  __shared__ float sm_top[4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int both = blockIdx.x / a.head_groups, head = (blockIdx.x - both * a.head_groups) * 4 + wave;
-  if (head >= a.nh) return;
+  const int both = blockIdx.x / a.nh, head = blockIdx.x - both * a.nh;
   const int unit = both >> 1, which = both & 1;   // K and V next to each other, as they lie in the projection's rows
   const int i = unit / a.slots, k = unit - i * a.slots;
   const int sid = a.at.seq_ids ? a.at.seq_ids[i] : i;
@@ -186,28 +193,27 @@ __global__ __launch_bounds__(256, 4) void kv_append_i8_kernel(AppendI8Args a) {
   const int64_t ph = (int64_t)page * a.nh + head;
   int8_t* codes = a.codes[which] + ph * (FG_PAGE_ROWS * DH);
   float* scale = a.scales[which] + ph;
-  auto store = [&](int j, int64_t p) {
-    const int64_t first = p > s0 ? p : s0;   // first position of row block j inside this page
-    const int lo = (int)(first - s0), hi = (int)(p + a.s < s0 + 64 ? p + a.s - s0 : 64);
-    const half_t* src = a.src[which] + ((int64_t)j * a.s + (first - p)) * a.ld + (int64_t)head * DH;
-    if (which == 0)
-      store_rows<DH, false>(src, a.ld, codes, scale, lo, hi, lane, sm[wave]);
-    else
-      store_rows<DH, true>(src, a.ld, codes, scale, lo, hi, lane, sm[wave]);
-  };
-  // A sequence that is named more than once: the first of its rows that touches the page stores them all, in order.
+  // A sequence that is named more than once: the first of its rows that touches the page stores them all, in order.  (Everything
+  // that decides is the same in all four waves.)
   const int from = a.at.seq_ids ? 0 : i, to = a.at.seq_ids ? a.b : i + 1;
   for (int base = from; base < to; base += 64) {
-    const int j = base + lane;
-    int64_t p = -1;
-    if (j < to && (!a.at.seq_ids || a.at.seq_ids[j] == sid)) p = a.at.pos ? a.at.pos[j] : 0;
-    uint64_t m = __builtin_amdgcn_ballot_w64(p >= 0 && p < s0 + 64 && p + a.s > s0);
+    const int jl = base + lane;
+    int64_t pl = -1;
+    if (jl < to && (!a.at.seq_ids || a.at.seq_ids[jl] == sid)) pl = a.at.pos ? a.at.pos[jl] : 0;
+    uint64_t m = __builtin_amdgcn_ballot_w64(pl >= 0 && pl < s0 + 64 && pl + a.s > s0);
     while (m) {
-      const int l = __builtin_ctzll(m);
+      const int l = __builtin_ctzll(m), j = base + l;
       m &= m - 1;
-      if (base + l < i) return;
-      store(base + l, __builtin_amdgcn_readlane((int)p, l));
-      __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");   // the next one's lanes read what these wrote
+      if (j < i) return;
+      const int64_t p = __builtin_amdgcn_readlane((int)pl, l);
+      const int64_t first = p > s0 ? p : s0;   // first position of row block j inside this page
+      const int lo = (int)(first - s0), hi = (int)(p + a.s < s0 + 64 ? p + a.s - s0 : 64);
+      const half_t* src = a.src[which] + ((int64_t)j * a.s + (first - p)) * a.ld + (int64_t)head * DH;
+      if (which == 0)
+        store_rows<DH, false>(src, a.ld, codes, scale, lo, hi, lane, wave, sm[wave], sm_top);
+      else
+        store_rows<DH, true>(src, a.ld, codes, scale, lo, hi, lane, wave, sm[wave], sm_top);
+      __syncthreads();   // the next one's waves read what these wrote
     }
   }
 }
@@ -422,8 +428,7 @@ int kv_append_i8_launch(const fg_model_cfg& cfg, const half_t* k, const half_t* 
     FG_LAUNCH_CHECK();
     return FG_OK;
   }
-  a.head_groups = (int)ceil_div(cfg.nh, 4);
-  const int64_t blocks = (int64_t)b * a.slots * a.head_groups * 2;
+  const int64_t blocks = (int64_t)b * a.slots * cfg.nh * 2;
   if (blocks > 0x7fffffff) return FG_ERR_SHAPE;
   const dim3 grid((unsigned)blocks);
   if (dh == 128)
