@@ -19,8 +19,8 @@ namespace {
 // taken one after the other instead.  Values carry their place in the key, so no two are equal.
 //
 // The sum of exponentials decides between words of different beams and so is kept better than one binary32 exponential is:
-// exp(y) = 2^h (1 + ln 2 l), y = x - max, with h + l = y log2 e to twice the precision; added up in binary32 over a thread's 8 or
-// 32 values and in binary64 from there on.  What is left are the roundings of y (none for words within a factor of two of the
+// exp(y) = 2^h (1 + (y - h ln 2)), y = x - max, h about y log2 e and ln 2 to twice the precision; added up in binary32 over a
+// thread's 8 or 32 values and in binary64 from there on.  What is left are the roundings of y (none for words within a factor of two of the
 // largest) and of the exponential instruction itself, some 2^-24 of each word's share and of either sign.
 constexpr int kList = 512;
 
@@ -62,9 +62,9 @@ template <int CTRL>
 __device__ __forceinline__ Key1 dpp(Key1 a) { return {dpp64<CTRL>(a.k)}; }
 template <int CTRL>
 __device__ __forceinline__ Key2 dpp(Key2 a) { return {dpp64<CTRL>(a.v), dpp64<CTRL>(a.k)}; }
-// over the wave, in registers: inside 16 lanes by DPP, then across
+// in registers: over each 16 lanes by DPP, then over the wave
 template <class Op>
-__device__ __forceinline__ double wave_f64(double v, Op op) {
+__device__ __forceinline__ double row16_f64(double v, Op op) {
   auto in16 = [&](auto ctrl) {
     constexpr int c = decltype(ctrl)::value;
     v = op(v, __builtin_bit_cast(double, dpp64<c>(__builtin_bit_cast(uint64_t, v))));
@@ -73,6 +73,11 @@ __device__ __forceinline__ double wave_f64(double v, Op op) {
   in16(std::integral_constant<int, kDppXor2>{});
   in16(std::integral_constant<int, kDppHalfMirror>{});
   in16(std::integral_constant<int, kDppMirror>{});
+  return v;
+}
+template <class Op>
+__device__ __forceinline__ double wave_f64(double v, Op op) {
+  v = row16_f64(v, op);
   auto pair = [&](const auto lo, const auto hi) {
     v = op(__builtin_bit_cast(double, (uint64_t)(uint32_t)hi[0] << 32 | (uint32_t)lo[0]),
            __builtin_bit_cast(double, (uint64_t)(uint32_t)hi[1] << 32 | (uint32_t)lo[1]));
@@ -88,8 +93,11 @@ __device__ __forceinline__ double wave_f64(double v, Op op) {
 __device__ __forceinline__ double wave_sum_f64(double v) {
   return wave_f64(v, [](double a, double b) { return a + b; });
 }
-__device__ __forceinline__ double wave_max_f64(double v) {
-  return wave_f64(v, [](double a, double b) { return fmax(a, b); });
+__device__ __forceinline__ double row16_sum_f64(double v) {
+  return row16_f64(v, [](double a, double b) { return a + b; });
+}
+__device__ __forceinline__ double row16_max_f64(double v) {
+  return row16_f64(v, [](double a, double b) { return fmax(a, b); });
 }
 template <class K>
 __device__ __forceinline__ K larger(K a, K b) { return a < b ? b : a; }
@@ -203,25 +211,30 @@ __global__ __launch_bounds__(256) void beam_rows_kernel(SelectArgs a) {
       x[j] = w < n ? src[w] : -INFINITY;
     }
   }
+  bool odd = false;
+#pragma unroll
+  for (int j = 0; j < VPT; ++j) odd = odd || __builtin_amdgcn_classf(x[j], 0x203);   // NaN or +inf
+  if (__builtin_amdgcn_ballot_w64(odd) != 0) {
+#pragma unroll
+    for (int j = 0; j < VPT; ++j) x[j] = clean(x[j]);
+  }
   float top = -INFINITY;
 #pragma unroll
-  for (int j = 0; j < VPT; ++j) {
-    x[j] = clean(x[j]);
-    top = fmaxf(top, x[j]);
-  }
+  for (int j = 0; j < VPT; j += 2) __asm__("v_max3_f32 %0, %1, %2, %0" : "+v"(top) : "v"(x[j]), "v"(x[j + 1]));
   const float wt = wave_max(top);
   if ((tid & 63) == 0) wave_top[tid >> 6] = wt;
   __syncthreads();
   const float m = fmaxf(fmaxf(wave_top[0], wave_top[1]), fmaxf(wave_top[2], wave_top[3]));
   const int64_t rp = (int64_t)row * a.pieces + blockIdx.x;
-  constexpr float L = 1.44269502f, Ll = 1.92596299e-8f;   // log2 e in two binary32 numbers
+  constexpr float ln2 = 0.693147182f, ln2_rest = -1.90465421e-9f;   // in two binary32 numbers
   float s = 0.f;
 #pragma unroll
   for (int j = 0; j < VPT; ++j) {
     const float y = fmaxf(x[j] - m, -150.f);   // 2^-216 is 0; a piece without words (-inf - -inf) comes here too
-    const float h = y * L, l = __builtin_fmaf(y, Ll, __builtin_fmaf(y, L, -h));
+    const float h = y * 1.44269502f, rest = __builtin_fmaf(h, -ln2_rest, __builtin_fmaf(h, -ln2, y));
     const float e = __builtin_amdgcn_exp2f(h);
-    s += __builtin_fmaf(e, l * 0.693147181f, e);
+    s += e;
+    s = __builtin_fmaf(e, rest, s);
   }
   const double d = wave_sum_f64((double)s);
   if ((tid & 63) == 0) part[tid >> 6] = d;
@@ -236,7 +249,10 @@ __global__ __launch_bounds__(256) void beam_rows_kernel(SelectArgs a) {
         const float lx = least.none() ? -INFINITY : from_ordered((uint32_t)(least.k >> 32));
 #pragma unroll
         for (int j = 0; j < VPT; ++j)
-          if (x[j] >= lx) f(key(j));
+          if (x[j] >= lx) {
+            __asm__ volatile("");   // few words come here: their keys are not made for all the others as well
+            f(key(j));
+          }
       },
       [&](int place, Key1 k) { a.best[rp * a.n_best + place] = k.k; });
   if (tid >= found && tid < a.n_best) a.best[rp * a.n_best + tid] = 0;
@@ -255,7 +271,7 @@ __global__ __launch_bounds__(256) void beam_merge_kernel(SelectArgs a) {
   __shared__ double lse[FG_MAX_BEAMS], score[FG_MAX_BEAMS];
   __shared__ int state[FG_MAX_BEAMS];   // 0: out, 1: alive, 2: done
   __shared__ int count;
-  const int g = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+  const int g = blockIdx.x, tid = threadIdx.x;
   const int64_t row0 = (int64_t)g * a.beams;
   const int per_beam = a.pieces * a.n_best, total = a.beams * per_beam;
   const uint64_t* best = a.best + row0 * per_beam;
@@ -265,25 +281,25 @@ __global__ __launch_bounds__(256) void beam_merge_kernel(SelectArgs a) {
 #pragma unroll
     for (int i = 0; i < kHeld / 256; ++i) raw[i] = tid + 256 * i < total ? best[tid + 256 * i] : 0;
   }
-  for (int j = tid >> 6; j < a.beams; j += 4) {   // a wave per beam
-    const bool over = a.done && a.done[row0 + j];
-    const float sc = a.scores[row0 + j];
-    const int64_t rp = (row0 + j) * a.pieces;
+  static_assert(FG_MAX_BEAMS * 16 <= 256, "sixteen lanes per beam");
+  const int j16 = tid >> 4, lane16 = tid & 15;
+  if (j16 < a.beams) {
+    const bool over = a.done && a.done[row0 + j16];
+    const float sc = a.scores[row0 + j16];
+    const int64_t rp = (row0 + j16) * a.pieces;
     double ref = -INFINITY, s = 0.0;
-    if (!over) {
-      for (int p0 = 0; p0 < a.pieces; p0 += 64) {
-        const int p = p0 + lane;
-        const double sp = p < a.pieces ? a.sums[rp + p] : 0.0, rf = p < a.pieces ? a.refs[rp + p] : 0.0;
-        const double now = fmax(ref, wave_max_f64(sp > 0.0 ? rf : -INFINITY));
-        if (p0 > 0 && ref > -INFINITY) s *= exp(ref - now);   // over 64 pieces
-        s += wave_sum_f64(sp > 0.0 ? sp * exp(rf - now) : 0.0);
-        ref = now;
-      }
+    for (int p0 = 0; p0 < a.pieces; p0 += 16) {   // (of a beam that is done, nobody wrote these; nobody looks at what comes of them)
+      const int p = p0 + lane16;
+      const double sp = p < a.pieces ? a.sums[rp + p] : 0.0, rf = p < a.pieces ? a.refs[rp + p] : 0.0;
+      const double now = fmax(ref, row16_max_f64(sp > 0.0 ? rf : -INFINITY));
+      if (p0 > 0 && ref > -INFINITY) s *= exp(ref - now);
+      s += row16_sum_f64(sp > 0.0 ? sp * exp(rf - now) : 0.0);
+      ref = now;
     }
-    if (lane == 0) {
-      lse[j] = s > 0.0 ? ref + log(s) : 0.0;
-      score[j] = sc;
-      state[j] = !(sc > -INFINITY) ? 0 : (over ? 2 : 1);
+    if (lane16 == 0) {
+      lse[j16] = !over && s > 0.0 ? ref + log(s) : 0.0;
+      score[j16] = sc;
+      state[j16] = !(sc > -INFINITY) ? 0 : (over ? 2 : 1);
     }
   }
   __syncthreads();
