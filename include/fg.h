@@ -368,6 +368,13 @@ int fg_decode_layer_paged(const fg_model_cfg* cfg, const fg_layer_weights* wts, 
                           int32_t topk, const fg_kv_pages* pages, const fg_ragged* seqs, void* x_out, void* ws,
                           size_t ws_bytes, void* stream);
 
+/* fg_decode_layer_paged (topk = 0) for beam search: rows i*beams .. i*beams + beams-1 are expected to share pages, and on 8-bit
+ * pages (FG_I8P64) the attention reads a shared page once for all of them (fg_decode_attention_beams_paged); with other formats it
+ * is fg_decode_layer_paged.  b % beams == 0, 1 <= beams <= FG_MAX_BEAMS. */
+int fg_decode_layer_beams_paged(const fg_model_cfg* cfg, const fg_layer_weights* wts, const void* x_in, int32_t b,
+                                int32_t beams, const fg_kv_pages* pages, const fg_ragged* seqs, void* x_out, void* ws,
+                                size_t ws_bytes, void* stream);
+
 /* fg_prefill_layer storing the s K/V rows of sequence seq_ids[i] at positions 0 .. s-1 of its pages
  * (seqs->pos is ignored).  ws >= fg_layer_workspace_bytes(cfg, wts, b*s). */
 int fg_prefill_layer_paged(const fg_model_cfg* cfg, const fg_layer_weights* wts, const void* x_in, int32_t b,

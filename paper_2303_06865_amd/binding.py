@@ -131,6 +131,9 @@ EXPORTS = {
     "fg_decode_layer_paged": (C.c_int, [C.POINTER(fg_model_cfg), C.POINTER(fg_layer_weights), C.c_void_p, C.c_int32,
                                         C.c_int32, C.POINTER(fg_kv_pages), C.POINTER(fg_ragged), C.c_void_p, C.c_void_p,
                                         C.c_size_t, C.c_void_p]),
+    "fg_decode_layer_beams_paged": (C.c_int, [C.POINTER(fg_model_cfg), C.POINTER(fg_layer_weights), C.c_void_p, C.c_int32,
+                                              C.c_int32, C.POINTER(fg_kv_pages), C.POINTER(fg_ragged), C.c_void_p, C.c_void_p,
+                                              C.c_size_t, C.c_void_p]),
     "fg_decode_attention_topk_paged": (C.c_int, [C.POINTER(fg_model_cfg), C.c_void_p, C.c_int64, C.c_int32, C.c_int32,
                                                  C.POINTER(fg_kv_pages), C.POINTER(fg_ragged), C.c_int32, C.c_void_p,
                                                  C.c_void_p, C.c_void_p]),
@@ -612,13 +615,20 @@ def fg_decode_attention_topk_paged(cfg: Cfg, q: torch.Tensor, q_row_stride: int,
 
 def fg_decode_layer_paged(cfg: Cfg, w: LayerWeights, x: torch.Tensor, pages: KVPages, seqs: Ragged,
                           ws: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
-                          topk: int = 0) -> torch.Tensor:
+                          topk: int = 0, beams: int = 1) -> torch.Tensor:
+    """beams > 1 (fg_decode_layer_beams_paged): each `beams` rows in turn are expected to share pages; no topk."""
     x = _f16(x)
     b = x.shape[0]
     if out is None:
         out = torch.empty_like(x)
     if ws is None:
         ws = _ws(lib().fg_layer_workspace_bytes(C.byref(cfg.c), C.byref(w.c), b))
+    if beams != 1:
+        assert topk == 0
+        _check(lib().fg_decode_layer_beams_paged(C.byref(cfg.c), C.byref(w.c), _p(x), b, beams, C.byref(pages.c),
+                                                 C.byref(seqs.c), _p(out), _p(ws), ws.numel(), _stream()),
+               "fg_decode_layer_beams_paged")
+        return out
     _check(lib().fg_decode_layer_paged(C.byref(cfg.c), C.byref(w.c), _p(x), b, topk, C.byref(pages.c), C.byref(seqs.c),
                                        _p(out), _p(ws), ws.numel(), _stream()), "fg_decode_layer_paged")
     return out

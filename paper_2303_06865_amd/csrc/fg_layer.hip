@@ -256,6 +256,7 @@ static LayerWs carve_layer_ws(const fg_model_cfg& c, const fg_layer_weights& w, 
 struct PagedKv {
   const fg_kv_pages* pages;
   const fg_ragged* seqs;
+  int32_t beams = 1;   // rows in turn that are expected to share pages
 };
 static int run_layer(const fg_model_cfg& c, const fg_layer_weights& w, const half_t* x_in, int32_t b, int32_t s,
                      bool prefill, int32_t t, const fg_kv_cache& kv, int32_t batch_offset, half_t* x_out,
@@ -285,7 +286,7 @@ static int run_layer(const fg_model_cfg& c, const fg_layer_weights& w, const hal
         rc = decode_attention_topk_paged_launch(c, L.qkv, 3 * h1, b, topk, *paged->pages, *paged->seqs, 1, L.o,
                                                 nullptr, st);
       else if (paged->pages->dtype == FG_I8P64)   // the buffers from act on are free here
-        rc = decode_attention_i8_launch(c, c.nh, 1, L.qkv, 3 * h1, b, *paged->pages, *paged->seqs, 1, L.o, L.act,
+        rc = decode_attention_i8_launch(c, c.nh, paged->beams, L.qkv, 3 * h1, b, *paged->pages, *paged->seqs, 1, L.o, L.act,
                                         L.total - (reinterpret_cast<unsigned char*>(L.act) - reinterpret_cast<unsigned char*>(ws)), st);
       else
         rc = decode_attention_paged_launch(c, L.qkv, 3 * h1, b, *paged->pages, *paged->seqs, 1, L.o, st);
@@ -598,7 +599,7 @@ extern "C" int fg_decode_layer(const fg_model_cfg* cfg, const fg_layer_weights* 
 
 static int paged_layer_entry(const fg_model_cfg* cfg, const fg_layer_weights* wts, const void* x_in, int32_t b,
                              int32_t s, bool prefill, const fg_kv_pages* pages, const fg_ragged* seqs, void* x_out,
-                             void* ws, size_t ws_bytes, void* stream, int32_t topk = 0) {
+                             void* ws, size_t ws_bytes, void* stream, int32_t topk = 0, int32_t beams = 1) {
   if (!cfg || !wts) return FG_ERR_NULL;
   int rc = check_cfg(cfg);
   if (rc) return rc;
@@ -606,6 +607,7 @@ static int paged_layer_entry(const fg_model_cfg* cfg, const fg_layer_weights* wt
   if ((rc = check_pages(cfg, pages, seqs))) return rc;
   if (!prefill && !seqs->pos) return FG_ERR_NULL;
   if (b < 0 || s < 0 || b > 65535 || (int64_t)b * s > 0x7fffffff || topk < 0) return FG_ERR_SHAPE;
+  if (beams < 1 || beams > FG_MAX_BEAMS || b % beams != 0) return FG_ERR_SHAPE;
   if (topk > 0 && pages->dtype != FG_Q4G64 && pages->dtype != FG_Q4G64_H16) return FG_ERR_UNSUPPORTED;
   if (topk > 0 && ((int64_t)seqs->table_stride * FG_PAGE_ROWS + 127) / 128 * 128 + topk > 36864) return FG_ERR_UNSUPPORTED;
   if (prefill && s > (int64_t)seqs->table_stride * FG_PAGE_ROWS) return FG_ERR_SHAPE;
@@ -615,7 +617,7 @@ static int paged_layer_entry(const fg_model_cfg* cfg, const fg_layer_weights* wt
   const size_t need = carve_layer_ws(*cfg, *wts, (int64_t)b * s, nullptr).total;
   if (!ws || ws_bytes < need) return FG_ERR_WORKSPACE;
   if (!aligned16(ws)) return FG_ERR_SHAPE;
-  const PagedKv pk = {pages, seqs};
+  const PagedKv pk = {pages, seqs, beams};
   const fg_kv_cache none = {};
   return run_layer(*cfg, *wts, reinterpret_cast<const half_t*>(x_in), b, s, prefill, 0, none, 0,
                    reinterpret_cast<half_t*>(x_out), ws, ws_bytes, as_stream(stream), &pk, topk);
@@ -625,6 +627,12 @@ extern "C" int fg_decode_layer_paged(const fg_model_cfg* cfg, const fg_layer_wei
                                      int32_t b, int32_t topk, const fg_kv_pages* pages, const fg_ragged* seqs,
                                      void* x_out, void* ws, size_t ws_bytes, void* stream) {
   return paged_layer_entry(cfg, wts, x_in, b, 1, false, pages, seqs, x_out, ws, ws_bytes, stream, topk);
+}
+
+extern "C" int fg_decode_layer_beams_paged(const fg_model_cfg* cfg, const fg_layer_weights* wts, const void* x_in, int32_t b,
+                                           int32_t beams, const fg_kv_pages* pages, const fg_ragged* seqs, void* x_out,
+                                           void* ws, size_t ws_bytes, void* stream) {
+  return paged_layer_entry(cfg, wts, x_in, b, 1, false, pages, seqs, x_out, ws, ws_bytes, stream, 0, beams);
 }
 
 extern "C" int fg_prefill_layer_paged(const fg_model_cfg* cfg, const fg_layer_weights* wts, const void* x_in,

@@ -7,7 +7,7 @@ import torch
 from paper_2303_06865_amd import binding as B
 from paper_2303_06865_amd import synth
 from tests import plain_i8 as P
-from tests.util import dev, host
+from tests.util import assert_close, dev, host
 
 pytestmark = pytest.mark.gpu
 
@@ -289,7 +289,7 @@ class _Search:
         x = B.fg_embed_ragged(self.cfg, self.m["embed"], self.m["pos"], ids.contiguous(), self.pos)
         ragged = B.Ragged(self.table, None, self.pos)
         for w, pool in zip(self.layers, self.pools):
-            x = B.fg_decode_layer_paged(self.cfg, w, x, pool, ragged)
+            x = B.fg_decode_layer_paged(self.cfg, w, x, pool, ragged, beams=self.beams)
         self.pos += 1
         self.logits = self._head(x)
 
@@ -337,6 +337,38 @@ def test_beam_search_on_8_bit_pages_and_one_beam_is_greedy():
     m = one.m
     ids, _ = B.fg_generate_diagonal(one.cfg, one.layers, m["embed"], m["pos"], m["lnf_g"], m["lnf_b"], dev(prompts), 6, 2, pools)
     assert np.array_equal(host(ids), host(one.text)[:, 0])
+
+
+@pytest.mark.parametrize("fmt", ["i8", "f16", "q4"])
+def test_layer_of_beams_is_the_layer(fmt):
+    """Sharing pages changes what is read, not what comes out: 8-bit pages up to the order of sums (an FP16 step of the layer's
+    output at most, 2^-10 of its size, and what an FP16 step of the attention's output makes of it), the others bit for bit."""
+    cfg, layers, _ = _model()
+    beams, b, at = 4, 8, 150
+    stride, per = 3, 2 + 4 * 2
+    pos = np.full(b, at, np.int32)
+    table = _tree(2, beams, stride, pos, per, 3, 2)
+    outs = []
+    for shared in (1, beams):
+        pool = _pool(fmt, cfg, 2 * per, 5)
+        if fmt == "i8":
+            pool.k_meta.abs_().mul_(0.02)
+            pool.v_meta.abs_().mul_(0.02)
+        elif fmt == "q4":
+            pool.k_meta.mul_(0.1)
+            pool.v_meta.mul_(0.1)
+        x = dev(_logits(b, SH.h1, 1, 1.0).astype(np.float16))
+        outs.append(host(B.fg_decode_layer_paged(cfg, layers[0], x, pool, B.Ragged(dev(table), None, dev(pos)), beams=shared)))
+    if fmt == "i8":
+        assert_close(outs[1], outs[0], "beams")
+    else:
+        assert np.array_equal(outs[0], outs[1])
+    cfg_c, w = cfg.c, layers[0].c
+    seqs = B.Ragged(dev(table), None, dev(pos))
+    ws = torch.empty(1 << 26, dtype=torch.uint8, device="cuda")
+    call = lambda n, k: B.lib().fg_decode_layer_beams_paged(B.C.byref(cfg_c), B.C.byref(w), x.data_ptr(), n, k, B.C.byref(pool.c),  # noqa: E731
+                                                            B.C.byref(seqs.c), x.data_ptr(), ws.data_ptr(), ws.numel(), None)
+    assert call(8, 3) == call(8, 0) == call(8, 17) == B.FG_ERR_SHAPE and call(0, 4) == B.FG_OK
 
 
 def test_captured_step_replays():
