@@ -122,6 +122,7 @@ typedef struct {
  * FG_I8P64 pages: k_codes [n_pages][nh][64][dh] bytes; v_codes [n_pages][nh][4][dh][16] bytes (16 consecutive
  * positions of one head dimension lie next to each other: the order in which the matrix cores contract over
  * positions); k_meta/v_meta [n_pages][nh] binary32 scales (4-byte aligned).
+ * Their contents do not matter before a page's first position is stored.
  * In the other formats rows are stored exactly as in fg_kv_cache; only their place differs. */
 #define FG_PAGE_ROWS 64
 typedef struct {
@@ -338,7 +339,7 @@ int fg_decode_attention_paged(const fg_model_cfg* cfg, const void* q_f16, int64_
  * the beams of one sequence share those of its prompt: a page that several of them name for the same positions is
  * read once.  Results do not depend on `beams`, up to the order of sums; any mixture of shared and own pages is right.
  * ws (FG_ERR_WORKSPACE without it) holds the partial results of long sequences that are split over workgroups; sized
- * for b rows and tables of table_stride pages.  The other calls on 8-bit pages (fg_decode_attention_paged, the paged
+ * for b rows and tables of table_stride pages; one ws serves one call at a time.  The other calls on 8-bit pages (fg_decode_attention_paged, the paged
  * layers, fg_generate_diagonal) run the same kernel with beams = 1, nkv = nh. */
 #define FG_MAX_BEAMS 16
 int fg_decode_attention_beams_paged(const fg_model_cfg* cfg, int32_t nkv, int32_t beams, const void* q_f16,
@@ -422,7 +423,8 @@ int64_t fg_diagonal_pages_needed(int32_t n_seqs, int32_t s, int32_t n, int32_t g
  * `eos` (0 <= eos < vocab, else FG_ERR_SHAPE) at its own score, and its logits do not matter.
  * Outputs, [n_groups][n_best]: the beam 0 .. beams-1 continued, the word, its v, and (NULL: not wanted) out_done =
  * done of the beam, or word == eos (eos < 0: never).  Where there are fewer continuations than n_best, the rest are
- * beam -1, word -1, v = -inf, done 1.  ws >= fg_beam_select_workspace_bytes. */
+ * beam -1, word -1, v = -inf, done 1.  With n_best == beams, out_scores may be scores and out_done may be done (a search that
+ * keeps its state in place); no other overlaps.  ws >= fg_beam_select_workspace_bytes; one ws serves one call at a time. */
 #define FG_MAX_BEST 32
 int fg_beam_select(const fg_model_cfg* cfg, int32_t n_groups, int32_t beams, int32_t n_best, const float* logits,
                    int64_t row_stride, const float* scores, const int32_t* done, int32_t eos, int32_t* out_beams,
@@ -436,13 +438,14 @@ size_t fg_beam_select_workspace_bytes(const fg_model_cfg* cfg, int32_t n_groups,
  * if it is partly filled, the first row of the group that holds it keeps it and the others take a free page and a copy
  * of its filled rows (up to the next multiple of 16) in every layer; if it is not begun, every row takes a free page.
  * Group g owns pages g*pages_per_group .. (g+1)*pages_per_group - 1 of the pools (all below n_pages); free are those
- * that no row of the group holds any more, and the lowest is taken first.  Pages outside the group's range (a prompt
+ * that no row of the group holds any more, and the lowest is taken first (so nobody else may hold pages of that range).  Pages outside the group's range (a prompt
  * shared between groups) are only read: a row whose partly filled page lies there takes a copy.  A row that finds no
  * free page, or whose next position is beyond the table, gets no entry there (-1: appending skips it) and counts in
  * missing[g] (int32 per group, or NULL).  pages_per_group = pages of the prompt + beams * (own pages per beam + 1)
  * always suffices.
  * table_in, pos_in, parents, table_out [rows][table_stride], pos_out: device int32, rows = n_groups * beams; table_out
- * may be table_in and pos_out pos_in, other overlaps are not allowed.  ws >= fg_beam_reorder_workspace_bytes. */
+ * may be table_in and pos_out pos_in, other overlaps are not allowed.  ws >= fg_beam_reorder_workspace_bytes; one ws serves one call at a
+ * time. */
 int fg_beam_reorder_paged(const fg_model_cfg* cfg, int32_t l, const fg_kv_pages* pages, int32_t n_groups, int32_t beams,
                           int32_t pages_per_group, const int32_t* parents, const int32_t* table_in,
                           const int32_t* pos_in, int32_t table_stride, int32_t* table_out, int32_t* pos_out,

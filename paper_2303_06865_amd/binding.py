@@ -190,7 +190,13 @@ def _check(status: int, where: str) -> None:
         raise FgError(status, where)
 
 
+# the current stream's handle without a Stream object around it (2 us of a small call), where torch offers it
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream() -> int:
+    if _raw_stream is not None:
+        return _raw_stream(torch.cuda.current_device())
     return torch.cuda.current_stream().cuda_stream
 
 
@@ -518,6 +524,13 @@ def fg_decode_attention_paged(cfg: Cfg, q: torch.Tensor, q_row_stride: int, b: i
     return out
 
 
+def _on_this_device(*tensors: Optional[torch.Tensor]) -> None:
+    """The launches go to the current device's stream."""
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        assert t is None or t.get_device() == dev, "tensors have to be on the current device"
+
+
 def decode_attention_beams_workspace(cfg: Cfg, nkv: int, beams: int, b: int, table_stride: int) -> torch.Tensor:
     return _ws(lib().fg_decode_attention_beams_workspace_bytes(C.byref(cfg.c), nkv, beams, b, table_stride))
 
@@ -526,6 +539,8 @@ def fg_decode_attention_beams_paged(cfg: Cfg, nkv: int, beams: int, q: torch.Ten
                                     pages: KVPages, seqs: Ragged, rows_bias: int = 0, ws: Optional[torch.Tensor] = None,
                                     out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Attention of b rows over 8-bit pages of nkv heads; each `beams` rows in turn share the pages that their tables share."""
+    assert q.dtype == torch.float16 and pages.k_codes.shape[1] == nkv
+    _on_this_device(q, out, ws, pages.k_codes)
     if out is None:
         out = torch.empty((b, cfg.h1), dtype=torch.float16, device=q.device)
     if ws is None:
@@ -539,6 +554,9 @@ def fg_decode_attention_beams_paged(cfg: Cfg, nkv: int, beams: int, q: torch.Ten
 def fg_kv_gather_paged(cfg: Cfg, pages: KVPages, seqs: Ragged, b: int, s: int, k_out: Optional[torch.Tensor] = None,
                        v_out: Optional[torch.Tensor] = None, row_stride: Optional[int] = None):
     """Positions pos[i] .. pos[i] + s - 1 of sequence seq_ids[i] as FP16 (k, v), [b, s, h1]."""
+    assert pages.k_codes.shape[1] == cfg.nh
+    _on_this_device(pages.k_codes, k_out, v_out)
+    assert k_out is None or k_out.dtype == v_out.dtype == torch.float16
     if k_out is None:
         k_out = torch.empty((b, s, cfg.h1), dtype=torch.float16, device=pages.k_codes.device)
         v_out = torch.empty_like(k_out)
@@ -553,19 +571,23 @@ def beam_select_workspace(cfg: Cfg, n_groups: int, beams: int, n_best: int) -> t
 
 
 def fg_beam_select(cfg: Cfg, logits: torch.Tensor, scores: torch.Tensor, beams: int, n_best: Optional[int] = None,
-                   done: Optional[torch.Tensor] = None, eos: int = -1, ws: Optional[torch.Tensor] = None):
+                   done: Optional[torch.Tensor] = None, eos: int = -1, ws: Optional[torch.Tensor] = None, inplace: bool = False):
     """logits float32 [n * beams, vocab] (rows may be apart), scores float32 [n * beams], done int32 [n * beams] or None.
-    Returns (beams int32, ids int32, scores float32, done int32), each [n, n_best], best first."""
-    assert logits.dtype == torch.float32 and logits.is_cuda and logits.dim() == 2 and logits.stride(1) == 1
-    assert logits.shape[1] == cfg.vocab
-    rows = logits.shape[0]
-    assert scores.dtype == torch.float32 and scores.is_cuda and scores.is_contiguous() and scores.numel() == rows
-    assert done is None or (done.dtype == torch.int32 and done.is_cuda and done.is_contiguous() and done.numel() == rows)
+    Returns (beams int32, ids int32, scores float32, done int32), each [n, n_best], best first; inplace (n_best == beams): the
+    last two are written over scores and done."""
+    rows, vocab = logits.shape
+    assert logits.dtype == torch.float32 and logits.stride(1) == 1 and vocab == cfg.vocab
+    assert scores.dtype == torch.float32 and scores.is_contiguous() and scores.numel() == rows
+    assert done is None or (done.dtype == torch.int32 and done.is_contiguous() and done.numel() == rows)
     assert rows % beams == 0
+    _on_this_device(logits, scores, done, ws)
     n_best = beams if n_best is None else n_best
     n = rows // beams
     out_beams, ids, out_done = (torch.empty((n, n_best), dtype=torch.int32, device=logits.device) for _ in range(3))
     out = torch.empty((n, n_best), dtype=torch.float32, device=logits.device)
+    if inplace:
+        assert n_best == beams
+        out, out_done = scores.view(n, beams), out_done if done is None else done.view(n, beams)
     if ws is None:
         ws = beam_select_workspace(cfg, n, beams, n_best)
     _check(lib().fg_beam_select(C.byref(cfg.c), n, beams, n_best, _p(logits), max(logits.stride(0), cfg.vocab), _p(scores),
@@ -586,8 +608,10 @@ def fg_beam_reorder_paged(cfg: Cfg, pages: Sequence[KVPages], table: torch.Tenso
     (table, pos, missing int32 [n]); table_out = table and pos_out = pos rewrite them in place."""
     rows, stride = table.shape
     for t in (table, pos, parents, table_out, pos_out, missing):
-        assert t is None or (t.dtype == torch.int32 and t.is_cuda and t.is_contiguous())
+        assert t is None or (t.dtype == torch.int32 and t.is_contiguous())
     assert pos.numel() == rows and parents.numel() == rows and rows % beams == 0
+    assert pages[0].k_codes.shape[1] == cfg.nh
+    _on_this_device(table, pos, parents, table_out, pos_out, missing, ws, pages[0].k_codes)
     table_out = torch.empty_like(table) if table_out is None else table_out
     pos_out = torch.empty_like(pos) if pos_out is None else pos_out
     assert table_out.shape == table.shape and pos_out.numel() == rows

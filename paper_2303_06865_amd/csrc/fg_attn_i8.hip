@@ -417,7 +417,7 @@ int decode_attention_i8_launch(const fg_model_cfg& cfg, int32_t nkv, int32_t bea
   const int dh = cfg.h1 / cfg.nh;
   Plan p = plan_i8(cfg.nh, nkv, beams, b, seqs.table_stride);
   const int64_t rh = (int64_t)b * cfg.nh;
-  if (rh > 0x7fffffff) return FG_ERR_SHAPE;
+  if (rh > 0x7fffffff || ceil_div(p.units * p.wpu, 4) > kMostBlocks) return FG_ERR_SHAPE;
   while (p.splits > 1 && (!ws || ws_bytes < part_bytes(rh, p.splits, dh))) p.splits = ws ? p.splits - 1 : 1;
   AttnI8Args a;
   a.q = q;

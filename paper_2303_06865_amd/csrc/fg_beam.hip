@@ -600,7 +600,7 @@ extern "C" int fg_beam_reorder_paged(const fg_model_cfg* cfg, int32_t l, const f
   if (!cfg || !pages) return FG_ERR_NULL;
   int rc = check_cfg(cfg);
   if (rc) return rc;
-  if (l <= 0 || !groups_ok(n_groups, beams) || pages_per_group < 1 || table_stride < 1) return FG_ERR_SHAPE;
+  if (l <= 0 || !groups_ok(n_groups, beams) || n_groups > kMostBlocks || pages_per_group < 1 || table_stride < 1) return FG_ERR_SHAPE;
   if ((int64_t)table_stride * FG_PAGE_ROWS > 0x7fffffff) return FG_ERR_SHAPE;
   if (pages_per_group > kMostGroupPages) return FG_ERR_UNSUPPORTED;
   const fg_ragged seqs = {table_in ? table_in : parents, nullptr, nullptr, table_stride, 1};

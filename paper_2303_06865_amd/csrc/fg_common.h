@@ -53,6 +53,9 @@ struct ProfScope {
 
 static inline hipStream_t as_stream(void* s) { return reinterpret_cast<hipStream_t>(s); }
 
+// A launch counts its work items in 32 bits: workgroups of 256 threads that a grid can have
+constexpr int64_t kMostBlocks = 0xffffffffll / 256;
+
 static inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 static inline size_t align_up(size_t a, size_t b) { return (a + b - 1) / b * b; }
 

@@ -419,7 +419,7 @@ int kv_append_i8_launch(const fg_model_cfg& cfg, const half_t* k, const half_t* 
   ProfScope prof(FG_K_KV_APPEND, stream);
   if (s == 1) {
     const int hpw = 512 / dh;   // heads a wave
-    if (ceil_div(cfg.nh, 4 * hpw) > 65535) return FG_ERR_SHAPE;
+    if (b > kMostBlocks || ceil_div(cfg.nh, 4 * hpw) > 65535) return FG_ERR_SHAPE;
     const dim3 grid((unsigned)b, (unsigned)ceil_div(cfg.nh, 4 * hpw), 2);
     if (dh == 128)
       hipLaunchKernelGGL(kv_append_i8_row_kernel<128>, grid, dim3(256), 0, stream, a);
@@ -429,7 +429,7 @@ int kv_append_i8_launch(const fg_model_cfg& cfg, const half_t* k, const half_t* 
     return FG_OK;
   }
   const int64_t blocks = (int64_t)b * a.slots * cfg.nh * 2;
-  if (blocks > 0x7fffffff) return FG_ERR_SHAPE;
+  if ((int64_t)b * a.slots > kMostBlocks || blocks > kMostBlocks) return FG_ERR_SHAPE;
   const dim3 grid((unsigned)blocks);
   if (dh == 128)
     hipLaunchKernelGGL(kv_append_i8_kernel<128>, grid, dim3(256), 0, stream, a);
@@ -469,7 +469,7 @@ extern "C" int fg_kv_gather_paged(const fg_model_cfg* cfg, const fg_kv_pages* pa
   a.slots = seqs->pos ? (int)ceil_div((int64_t)s + 63, 64) : (int)ceil_div(s, 64);
   a.head_groups = (int)ceil_div(cfg->nh, 4);
   const int64_t blocks = (int64_t)b * a.slots * a.head_groups;
-  if (blocks > 0x7fffffff) return FG_ERR_SHAPE;
+  if ((int64_t)b * a.slots > kMostBlocks || blocks > kMostBlocks) return FG_ERR_SHAPE;
   const dim3 grid((unsigned)blocks, 2);
   hipStream_t st = as_stream(stream);
   ProfScope prof(FG_K_KV_GATHER, st);

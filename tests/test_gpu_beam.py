@@ -45,6 +45,19 @@ def test_select(vocab, n, beams, n_best):
     _check_select(x, scores, beams, n_best, None, eos=int(x[0].argmax()))
 
 
+def test_select_in_place():
+    x = _logits(12, 5003, 3)
+    r = np.random.default_rng(1)
+    scores, done = r.uniform(-9, 0, 12).astype(np.float32), (r.random(12) < 0.4).astype(np.int32)
+    cfg = B.Cfg(64, 1, 64, 5003, 64)
+    want = [host(t) for t in B.fg_beam_select(cfg, dev(x), dev(scores), 4, done=dev(done), eos=9)]
+    ds, dd = dev(scores), dev(done)
+    got = B.fg_beam_select(cfg, dev(x), ds, 4, done=dd, eos=9, inplace=True)
+    for a, b in zip(got, want):
+        assert np.array_equal(host(a), b)
+    assert np.array_equal(host(ds), want[2].reshape(-1)) and np.array_equal(host(dd), want[3].reshape(-1))
+
+
 def test_select_ties_and_forbidden_words():
     """Equal logits in a row, equal rows, rows without a word, -inf, NaN and +inf; more wanted than there are."""
     vocab = 3000
@@ -341,8 +354,8 @@ def test_beam_search_on_8_bit_pages_and_one_beam_is_greedy():
 
 @pytest.mark.parametrize("fmt", ["i8", "f16", "q4"])
 def test_layer_of_beams_is_the_layer(fmt):
-    """Sharing pages changes what is read, not what comes out: 8-bit pages up to the order of sums (an FP16 step of the layer's
-    output at most, 2^-10 of its size, and what an FP16 step of the attention's output makes of it), the others bit for bit."""
+    """Sharing pages changes what is read, not what comes out: 8-bit pages up to the order of sums (within the suite's bar for
+    activations), the others bit for bit."""
     cfg, layers, _ = _model()
     beams, b, at = 4, 8, 150
     stride, per = 3, 2 + 4 * 2
