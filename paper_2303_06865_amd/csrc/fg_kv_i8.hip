@@ -289,108 +289,90 @@ struct GatherArgs {
   const void* meta[2];
   half_t* out[2];
   int64_t ld;
-  int32_t b, s, nh, slots, head_groups;
+  int32_t b, s, nh, slots;
   PageRows at;
 };
 
-// One wave per (sequence of the call, page, head, K or V), four groups of 16 positions one after the other; lane = 8 head
-// dimensions (lane % LR) of RPL positions of the group.  All loads go out before the first value is used, and groups that
-// nobody asked for are skipped.  The 8-bit value codes come in their units, in order, and pass through LDS.
+// One workgroup per (sequence of the call, page, head, K or V), a wave per group of 16 positions; lane = 8 head dimensions
+// (lane % LR) of RPL positions.  Waves whose group nobody asked for have nothing to do.  The 8-bit value codes come in their
+// units, in order, and pass through LDS.
 template <int DH, int FMT>
 __global__ __launch_bounds__(256) void kv_gather_kernel(GatherArgs a) {
-  constexpr int LR = DH / 8, RPL = LR / 4, UPL = DH / 64;   // positions of a group, units of a group per lane
+  constexpr int LR = DH / 8, RPL = LR / 4, UPL = DH / 64;   // positions, units per lane
   constexpr bool I8 = FMT == FG_I8P64, H16 = FMT == FG_Q4G64_H16;
   __shared__ __attribute__((aligned(16))) uint8_t sm[I8 ? 4 : 1][I8 ? 16 * DH : 16];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int unit = blockIdx.x / a.head_groups, head = (blockIdx.x - unit * a.head_groups) * 4 + wave;
-  if (head >= a.nh) return;
+  const int lane = threadIdx.x & 63, q = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int unit = blockIdx.x / a.nh, head = blockIdx.x - unit * a.nh;
   const int which = blockIdx.y;
   const int i = unit / a.slots, k = unit - i * a.slots;
   const int64_t p_i = a.at.pos ? a.at.pos[i] : 0;
   const int64_t slot = (p_i >> 6) + k, s0 = slot << 6;
-  if (s0 >= p_i + a.s) return;
-  const int page = page_at(a.at, a.at.seq_ids ? a.at.seq_ids[i] : i, slot);
   const int lo = p_i > s0 ? (int)(p_i - s0) : 0, hi = p_i + a.s < s0 + 64 ? (int)(p_i + a.s - s0) : 64;
-  const int d0 = (lane % LR) * 8, r0 = (lane / LR) * RPL;
+  if (16 * q >= hi || 16 * q + 16 <= lo) return;   // (behind the last row: hi <= 0)
+  const int page = page_at(a.at, a.at.seq_ids ? a.at.seq_ids[i] : i, slot);
+  const int d0 = (lane % LR) * 8, r_in = (lane / LR) * RPL, r0 = 16 * q + r_in;
   half_t* out = a.out[which] + ((int64_t)i * a.s + (s0 - p_i)) * a.ld + (int64_t)head * DH + d0;   // of the page's row 0
-  auto put = [&](int row, const h8_t v) {
-    if (row >= lo && row < hi) *reinterpret_cast<h8_t*>(out + (int64_t)row * a.ld) = v;
+  auto put = [&](int n, const h8_t v) {
+    if (r0 + n >= lo && r0 + n < hi) *reinterpret_cast<h8_t*>(out + (int64_t)(r0 + n) * a.ld) = v;
   };
   if (page < 0) {
-    for (int q = 0; q < 4; ++q)
 #pragma unroll
-      for (int n = 0; n < RPL; ++n) put(16 * q + r0 + n, (h8_t)(half_t)0);
+    for (int n = 0; n < RPL; ++n) put(n, (h8_t)(half_t)0);
     return;
   }
-  auto wanted = [&](int q) { return 16 * q < hi && 16 * q + 16 > lo; };   // the same in all lanes
   const int64_t ph = (int64_t)page * a.nh + head;
   if (I8 && which) {
-    const uint8_t* codes = reinterpret_cast<const uint8_t*>(a.codes[1]) + ph * (FG_PAGE_ROWS * DH);
+    const uint8_t* codes = reinterpret_cast<const uint8_t*>(a.codes[1]) + ph * (FG_PAGE_ROWS * DH) + q * (16 * DH);
     const float sc = reinterpret_cast<const float*>(a.meta[1])[ph];
-    u4_t u[4][UPL];
+    u4_t u[UPL];
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
-      if (wanted(q))
+    for (int t = 0; t < UPL; ++t) u[t] = *reinterpret_cast<const u4_t*>(codes + (64 * t + lane) * 16);
 #pragma unroll
-        for (int t = 0; t < UPL; ++t) u[q][t] = *reinterpret_cast<const u4_t*>(codes + (q * DH + 64 * t + lane) * 16);
+    for (int t = 0; t < UPL; ++t) *reinterpret_cast<u4_t*>(sm[q] + unit_at<DH>(0, 64 * t + lane)) = u[t];
+    wave_lds_fence();
+    uint32_t c[8];
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
-      if (wanted(q)) {
-        wave_lds_fence();
+    for (int e = 0; e < 8; ++e) {
+      const uint8_t* from = sm[q] + unit_at<DH>(0, d0 + e) + r_in;
+      c[e] = RPL == 4 ? *reinterpret_cast<const uint32_t*>(from) : *reinterpret_cast<const uint16_t*>(from);
+    }
 #pragma unroll
-        for (int t = 0; t < UPL; ++t) *reinterpret_cast<u4_t*>(sm[wave] + unit_at<DH>(0, 64 * t + lane)) = u[q][t];
-        wave_lds_fence();
-        uint32_t c[8];
+    for (int n = 0; n < RPL; ++n) {
+      h8_t v;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const uint8_t* from = sm[wave] + unit_at<DH>(0, d0 + e) + r0;
-          c[e] = RPL == 4 ? *reinterpret_cast<const uint32_t*>(from) : *reinterpret_cast<const uint16_t*>(from);
-        }
-#pragma unroll
-        for (int n = 0; n < RPL; ++n) {
-          h8_t v;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = to_half((float)(int8_t)(c[e] >> (8 * n)) * sc);
-          put(16 * q + r0 + n, v);
-        }
-      }
+      for (int e = 0; e < 8; ++e) v[e] = to_half((float)(int8_t)(c[e] >> (8 * n)) * sc);
+      put(n, v);
+    }
     return;
   }
   // rows in the order of their positions: raw[] = the lane's 8 elements as stored
   using raw_t = std::conditional_t<FMT == FG_F16, h8_t, std::conditional_t<I8, i8x8_t, uint32_t>>;
   using meta_t = std::conditional_t<H16, h2_t, float2>;
-  const raw_t* rows = reinterpret_cast<const raw_t*>(a.codes[which]) + ph * FG_PAGE_ROWS * LR + lane % LR;
+  const raw_t* rows = reinterpret_cast<const raw_t*>(a.codes[which]) + (ph * FG_PAGE_ROWS + r0) * LR + lane % LR;
   const float sc = I8 ? reinterpret_cast<const float*>(a.meta[which])[ph] : 0.f;
-  raw_t raw[4][RPL];
-  meta_t pair[4][FMT == FG_F16 || I8 ? 1 : RPL];
+  raw_t raw[RPL];
+  meta_t pair[FMT == FG_F16 || I8 ? 1 : RPL];
 #pragma unroll
-  for (int q = 0; q < 4; ++q)
-    if (wanted(q))
+  for (int n = 0; n < RPL; ++n) {
+    raw[n] = rows[n * LR];
+    if constexpr (FMT == FG_Q4G64 || H16)
+      pair[n] = reinterpret_cast<const meta_t*>(a.meta[which])[(ph * FG_PAGE_ROWS + r0 + n) * (DH / kGroup) + d0 / kGroup];
+  }
 #pragma unroll
-      for (int n = 0; n < RPL; ++n) {
-        const int row = 16 * q + r0 + n;
-        raw[q][n] = rows[row * LR];
-        if constexpr (FMT == FG_Q4G64 || H16)
-          pair[q][n] = reinterpret_cast<const meta_t*>(a.meta[which])[(ph * FG_PAGE_ROWS + row) * (DH / kGroup) + d0 / kGroup];
-      }
+  for (int n = 0; n < RPL; ++n) {
+    h8_t v;
+    if constexpr (FMT == FG_F16) {
+      v = raw[n];
+    } else if constexpr (I8) {
 #pragma unroll
-  for (int q = 0; q < 4; ++q)
-    if (wanted(q))
+      for (int e = 0; e < 8; ++e) v[e] = to_half((float)raw[n][e] * sc);
+    } else {
+      const float mn = (float)pair[n].x, step = (float)pair[n].y;
 #pragma unroll
-      for (int n = 0; n < RPL; ++n) {
-        h8_t v;
-        if constexpr (FMT == FG_F16) {
-          v = raw[q][n];
-        } else if constexpr (I8) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = to_half((float)raw[q][n][e] * sc);
-        } else {
-          const float mn = (float)pair[q][n].x, step = (float)pair[q][n].y;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = to_half(__builtin_fmaf((float)((raw[q][n] >> (4 * e)) & 15u), step, mn));
-        }
-        put(16 * q + r0 + n, v);
-      }
+      for (int e = 0; e < 8; ++e) v[e] = to_half(__builtin_fmaf((float)((raw[n] >> (4 * e)) & 15u), step, mn));
+    }
+    put(n, v);
+  }
 }
 
 }  // namespace
@@ -467,8 +449,7 @@ extern "C" int fg_kv_gather_paged(const fg_model_cfg* cfg, const fg_kv_pages* pa
   a.nh = cfg->nh;
   a.at = page_rows(*pages, *seqs, true);
   a.slots = seqs->pos ? (int)ceil_div((int64_t)s + 63, 64) : (int)ceil_div(s, 64);
-  a.head_groups = (int)ceil_div(cfg->nh, 4);
-  const int64_t blocks = (int64_t)b * a.slots * a.head_groups;
+  const int64_t blocks = (int64_t)b * a.slots * cfg->nh;
   if ((int64_t)b * a.slots > kMostBlocks || blocks > kMostBlocks) return FG_ERR_SHAPE;
   const dim3 grid((unsigned)blocks, 2);
   hipStream_t st = as_stream(stream);
