@@ -145,7 +145,7 @@ __device__ __forceinline__ int block_best(int n, K mine, K* list /* [kList] */, 
   K last = {};
   for (int p = 0; p < n; ++p) {   // more than n reach the bound: there is always a next one
     K best = {};
-    each(bound, [&](K k) {
+    each(K{}, [&](K k) {   // (all keys: asked again who reaches the bound, the compiler keeps the answers of the first time)
       if (!k.none() && (p == 0 || k < last) && best < k) best = k;
     });
     best = larger(best, dpp<kDppXor1>(best));
@@ -211,10 +211,16 @@ __global__ __launch_bounds__(256) void beam_rows_kernel(SelectArgs a) {
       x[j] = w < n ? src[w] : -INFINITY;
     }
   }
-  bool odd = false;
+  // Is there a NaN or +inf?  As whole numbers, +inf and the NaNs above it are the largest with a sign, and the NaNs with the
+  // sign set are above -inf without.
+  int most = 0;
+  uint32_t most_u = 0;
 #pragma unroll
-  for (int j = 0; j < VPT; ++j) odd = odd || __builtin_amdgcn_classf(x[j], 0x203);   // NaN or +inf
-  if (__builtin_amdgcn_ballot_w64(odd) != 0) {
+  for (int j = 0; j < VPT; j += 2) {
+    __asm__("v_max3_i32 %0, %1, %2, %0" : "+v"(most) : "v"(x[j]), "v"(x[j + 1]));
+    __asm__("v_max3_u32 %0, %1, %2, %0" : "+v"(most_u) : "v"(x[j]), "v"(x[j + 1]));
+  }
+  if (__builtin_amdgcn_ballot_w64(most >= 0x7f800000 || most_u > 0xff800000u) != 0) {
 #pragma unroll
     for (int j = 0; j < VPT; ++j) x[j] = clean(x[j]);
   }
