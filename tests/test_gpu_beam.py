@@ -102,6 +102,16 @@ def test_select_rows_apart_and_unaligned(shift):
     _check_select(x, np.zeros(rows, np.float32), 3, 6, logits=view)
 
 
+def test_select_rows_far_apart():
+    """Rows whose distance in elements passes 2^31 when multiplied out."""
+    vocab, ld = 1024, (1 << 30) + 64
+    big = torch.empty(2 * ld + vocab, device="cuda")
+    view = big.as_strided((3, vocab), (ld, 1))
+    x = _logits(3, vocab, 4)
+    view.copy_(dev(x))
+    _check_select(x, np.zeros(3, np.float32), 3, 6, logits=view)
+
+
 def test_select_sharp_and_flat_rows():
     """One word has nearly all the weight; all have the same; values far from zero."""
     vocab = 20000

@@ -235,6 +235,75 @@ def test_attention_of_ids_and_bad_tables():
     _check_attention(plain, table, q, lens, nh, nh, dh, got, np.array([3, 0, 1, 0]))
 
 
+@pytest.mark.parametrize("nh,nkv,b,beams,n,ws", [(1, 1, 2, 1, 17000, False), (1, 1, 132, 2, 16900, True), (1, 1, 1100, 1, 8700, True),
+                                                 (16, 1, 260, 1, 4300, True), (2, 2, 40, 4, 16700, True)])
+def test_attention_of_many_pages(nh, nkv, b, beams, n, ws):
+    """More pages than a wave keeps at once, at every number of waves a unit.  All sequences name the same few hundred pages (the
+    beams of a group differ in forty pages), so that some rows stand for all."""
+    dh = 64
+    stride = n // 64 + 1
+    plain = P.I8Pages(stride + 40 * beams, nkv, dh, seed=n)
+    r = np.random.default_rng(b)
+    one = r.permutation(plain.n)
+    table = np.empty((b, stride), np.int32)
+    for j in range(beams):
+        row = one[:stride].copy()
+        row[20:60] = one[stride + 40 * j:stride + 40 * (j + 1)]
+        table[j::beams] = row
+    q = _rows((b, nh * dh), 5)
+    cfg = _cfg(nh, dh)
+    pages = _upload(plain, B.Cfg(nkv * dh, nkv, 64, 64, 64))
+    seqs = B.Ragged(dev(table), None, dev(np.full(b, n, np.int32)))
+    if ws:
+        got = host(B.fg_decode_attention_beams_paged(cfg, nkv, beams, dev(q), nh * dh, b, pages, seqs))
+    else:
+        got = host(B.fg_decode_attention_paged(cfg, dev(q), nh * dh, b, pages, seqs))
+    rows = sorted({0, 1 % b, b // 2, b - 1} | set(range(min(beams, b))))
+    for i in rows:
+        _check_attention(plain, table[i:i + 1], q[i:i + 1], [n], nh, nkv, dh, got[i:i + 1])
+
+
+def test_pages_beyond_32_bits():
+    """Codes whose offsets pass 2^32: stored, read back, copied and attended to."""
+    nh, dh, cfg = 32, 128, _cfg(32, 128)
+    n_pages = (1 << 32) // (nh * 64 * dh) + 40
+    pages = B.KVPages(cfg, n_pages, int8=True, zero=False)
+    table = np.array([[n_pages - 1, n_pages - 2]], np.int32)
+    small = P.I8Pages(2, nh, dh)
+    kv = _rows((100, 2 * nh * dh), 1)
+    small.append(np.array([[0, 1]]), 0, 0, kv[:, :nh * dh], kv[:, nh * dh:])
+    d = dev(kv)
+    B.fg_kv_append_paged(cfg, d, d[:, nh * dh:], 2 * nh * dh, 1, 100, pages, B.Ragged(dev(table)))
+    k, v = B.fg_kv_gather_paged(cfg, pages, B.Ragged(dev(table)), 1, 100)
+    want = small.rows(np.array([[0, 1]]), 0, 100)
+    for got, x in zip((k, v), want):
+        assert np.array_equal(host(got)[0], x.astype(np.float32).astype(np.float16).transpose(1, 0, 2).reshape(100, -1))
+    two = dev(np.repeat(table, 2, 0))
+    pos = dev(np.array([100, 100], np.int32))
+    got_t, _, _ = B.fg_beam_reorder_paged(cfg, [pages], two, pos, dev(np.array([1, 0], np.int32)), 2, n_pages)
+    assert host(got_t).tolist() == [[n_pages - 1, n_pages - 2], [n_pages - 1, 0]]
+    q = _rows((2, nh * dh), 2)
+    out = B.fg_decode_attention_beams_paged(cfg, nh, 2, dev(q), nh * dh, 2, pages, B.Ragged(got_t, None, pos))
+    _check_attention(small, np.array([[0, 1], [0, 1]]), q, [100, 100], nh, nh, dh, host(out))
+
+
+def test_rows_past_the_table():
+    """Rows that run past the table's end are dropped when stored and read as zeros, also before position 0."""
+    nh, dh, cfg = 2, 128, _cfg(2, 128)
+    plain, table = P.I8Pages(5, nh, dh, seed=1), np.array([[4, 1]], np.int32)
+    pages = _upload(plain, cfg)
+    kv = _rows((70, 2 * nh * dh), 3)
+    plain.append(table, 0, 100, kv[:, :nh * dh], kv[:, nh * dh:])
+    d, at = dev(kv), lambda p: B.Ragged(dev(table), None, dev(np.array([p], np.int32)))
+    B.fg_kv_append_paged(cfg, d, d[:, nh * dh:], 2 * nh * dh, 1, 70, pages, at(100))
+    _same(pages, plain)
+    want = [x.astype(np.float32).astype(np.float16).transpose(1, 0, 2).reshape(128, -1) for x in plain.rows(table, 0, 128)]
+    k, v = (host(t)[0] for t in B.fg_kv_gather_paged(cfg, pages, at(120), 1, 80))
+    assert np.array_equal(k[:8], want[0][120:]) and np.array_equal(v[:8], want[1][120:]) and not k[8:].any() and not v[8:].any()
+    k, v = (host(t)[0] for t in B.fg_kv_gather_paged(cfg, pages, at(-70), 1, 90))
+    assert np.array_equal(k[70:], want[0][:20]) and np.array_equal(v[70:], want[1][:20]) and not k[:70].any() and not v[:70].any()
+
+
 def test_attention_extremes():
     """A score that dwarfs the others, a query of zeros, scales of zero, a page whose rows behind the end hold anything."""
     nh, dh, cfg = 4, 128, _cfg(4, 128)
