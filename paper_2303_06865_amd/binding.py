@@ -194,9 +194,10 @@ def _check(status: int, where: str) -> None:
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
-def _stream() -> int:
+def _stream(device: Optional[int] = None) -> int:
+    """device: the current device, where the caller has asked for it already."""
     if _raw_stream is not None:
-        return _raw_stream(torch.cuda.current_device())
+        return _raw_stream(torch.cuda.current_device() if device is None else device)
     return torch.cuda.current_stream().cuda_stream
 
 
@@ -524,11 +525,12 @@ def fg_decode_attention_paged(cfg: Cfg, q: torch.Tensor, q_row_stride: int, b: i
     return out
 
 
-def _on_this_device(*tensors: Optional[torch.Tensor]) -> None:
-    """The launches go to the current device's stream."""
+def _on_this_device(*tensors: Optional[torch.Tensor]) -> int:
+    """The current device, to whose stream the launches go: the tensors have to be there."""
     dev = torch.cuda.current_device()
     for t in tensors:
         assert t is None or t.get_device() == dev, "tensors have to be on the current device"
+    return dev
 
 
 def decode_attention_beams_workspace(cfg: Cfg, nkv: int, beams: int, b: int, table_stride: int) -> torch.Tensor:
@@ -540,13 +542,13 @@ def fg_decode_attention_beams_paged(cfg: Cfg, nkv: int, beams: int, q: torch.Ten
                                     out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Attention of b rows over 8-bit pages of nkv heads; each `beams` rows in turn share the pages that their tables share."""
     assert q.dtype == torch.float16 and pages.k_codes.shape[1] == nkv
-    _on_this_device(q, out, ws, pages.k_codes)
+    device = _on_this_device(q, out, ws, pages.k_codes)
     if out is None:
         out = torch.empty((b, cfg.h1), dtype=torch.float16, device=q.device)
     if ws is None:
         ws = decode_attention_beams_workspace(cfg, nkv, beams, b, seqs.page_table.shape[1])
     _check(lib().fg_decode_attention_beams_paged(C.byref(cfg.c), nkv, beams, _p(q), q_row_stride, b, C.byref(pages.c),
-                                                 C.byref(seqs.c), rows_bias, _p(out), _p(ws), ws.numel(), _stream()),
+                                                 C.byref(seqs.c), rows_bias, _p(out), _p(ws), ws.numel(), _stream(device)),
            "fg_decode_attention_beams_paged")
     return out
 
@@ -555,14 +557,14 @@ def fg_kv_gather_paged(cfg: Cfg, pages: KVPages, seqs: Ragged, b: int, s: int, k
                        v_out: Optional[torch.Tensor] = None, row_stride: Optional[int] = None):
     """Positions pos[i] .. pos[i] + s - 1 of sequence seq_ids[i] as FP16 (k, v), [b, s, h1]."""
     assert pages.k_codes.shape[1] == cfg.nh
-    _on_this_device(pages.k_codes, k_out, v_out)
+    device = _on_this_device(pages.k_codes, k_out, v_out)
     assert k_out is None or k_out.dtype == v_out.dtype == torch.float16
     if k_out is None:
         k_out = torch.empty((b, s, cfg.h1), dtype=torch.float16, device=pages.k_codes.device)
         v_out = torch.empty_like(k_out)
         row_stride = cfg.h1
     _check(lib().fg_kv_gather_paged(C.byref(cfg.c), C.byref(pages.c), C.byref(seqs.c), b, s, _p(k_out), _p(v_out),
-                                    row_stride, _stream()), "fg_kv_gather_paged")
+                                    row_stride, _stream(device)), "fg_kv_gather_paged")
     return k_out, v_out
 
 
@@ -580,7 +582,7 @@ def fg_beam_select(cfg: Cfg, logits: torch.Tensor, scores: torch.Tensor, beams: 
     assert scores.dtype == torch.float32 and scores.is_contiguous() and scores.numel() == rows
     assert done is None or (done.dtype == torch.int32 and done.is_contiguous() and done.numel() == rows)
     assert rows % beams == 0
-    _on_this_device(logits, scores, done, ws)
+    device = _on_this_device(logits, scores, done, ws)
     n_best = beams if n_best is None else n_best
     n = rows // beams
     out_beams, ids, out_done = (torch.empty((n, n_best), dtype=torch.int32, device=logits.device) for _ in range(3))
@@ -591,7 +593,7 @@ def fg_beam_select(cfg: Cfg, logits: torch.Tensor, scores: torch.Tensor, beams: 
     if ws is None:
         ws = beam_select_workspace(cfg, n, beams, n_best)
     _check(lib().fg_beam_select(C.byref(cfg.c), n, beams, n_best, _p(logits), max(logits.stride(0), cfg.vocab), _p(scores),
-                                _p(done), eos, _p(out_beams), _p(ids), _p(out), _p(out_done), _p(ws), ws.numel(), _stream()),
+                                _p(done), eos, _p(out_beams), _p(ids), _p(out), _p(out_done), _p(ws), ws.numel(), _stream(device)),
            "fg_beam_select")
     return out_beams, ids, out, out_done
 
@@ -611,7 +613,7 @@ def fg_beam_reorder_paged(cfg: Cfg, pages: Sequence[KVPages], table: torch.Tenso
         assert t is None or (t.dtype == torch.int32 and t.is_contiguous())
     assert pos.numel() == rows and parents.numel() == rows and rows % beams == 0
     assert pages[0].k_codes.shape[1] == cfg.nh
-    _on_this_device(table, pos, parents, table_out, pos_out, missing, ws, pages[0].k_codes)
+    device = _on_this_device(table, pos, parents, table_out, pos_out, missing, ws, pages[0].k_codes)
     table_out = torch.empty_like(table) if table_out is None else table_out
     pos_out = torch.empty_like(pos) if pos_out is None else pos_out
     assert table_out.shape == table.shape and pos_out.numel() == rows
@@ -622,7 +624,7 @@ def fg_beam_reorder_paged(cfg: Cfg, pages: Sequence[KVPages], table: torch.Tenso
     parr = (fg_kv_pages * len(pages))(*[p.c for p in pages])
     _check(lib().fg_beam_reorder_paged(C.byref(cfg.c), len(pages), parr, rows // beams, beams, pages_per_group, _p(parents),
                                        _p(table), _p(pos), stride, _p(table_out), _p(pos_out), _p(missing), _p(ws),
-                                       ws.numel(), _stream()), "fg_beam_reorder_paged")
+                                       ws.numel(), _stream(device)), "fg_beam_reorder_paged")
     return table_out, pos_out, missing
 
 
