@@ -340,7 +340,9 @@ int fg_decode_attention_paged(const fg_model_cfg* cfg, const void* q_f16, int64_
  * read once.  Results do not depend on `beams`, up to the order of sums; any mixture of shared and own pages is right.
  * ws (FG_ERR_WORKSPACE without it) holds the partial results of long sequences that are split over workgroups; sized
  * for b rows and tables of table_stride pages; one ws serves one call at a time.  The other calls on 8-bit pages (fg_decode_attention_paged, the paged
- * layers, fg_generate_diagonal) run the same kernel with beams = 1, nkv = nh. */
+ * layers, fg_generate_diagonal) run the same kernel with beams = 1, nkv = nh; fg_decode_attention_paged, which has no
+ * workspace, never splits a sequence (for a few long sequences this call is the faster one), the layers split as far as
+ * their own workspace reaches. */
 #define FG_MAX_BEAMS 16
 int fg_decode_attention_beams_paged(const fg_model_cfg* cfg, int32_t nkv, int32_t beams, const void* q_f16,
                                     int64_t q_row_stride, int32_t b, const fg_kv_pages* pages, const fg_ragged* seqs,
