@@ -20,8 +20,8 @@
 // Each keeps a running (maximum, sum, output) per column; they are merged through LDS, and through memory by a second launch
 // where there are splits.  A wave has the values of a page and the keys of its next one on their way while it computes.
 //
-// Bound by the loads where sequences are long: 64 sequences of 1 to 2047 rows, 32 heads of 128, 538 MB: 105 to 109 us, 5 TB/s; 16 x 4
-// beams of 512 shared and 30 own rows, 96 heads, 252 MB: 57 us; one sequence of 32768 rows, 32 heads on 8, 67 MB: 15 us and 4 for
+// Bound by the loads where sequences are long: 64 sequences of 1 to 2047 rows, 32 heads of 128, 538 MB: 105 us, 5 TB/s; 16 x 4
+// beams of 512 shared and 30 own rows, 96 heads, 252 MB: 51 us; one sequence of 32768 rows, 32 heads on 8, 67 MB: 15 us and 4 for
 // the merge.  A page costs a wave some 1700 cycles (64 conversions and additions for the scores, 16 exponentials, 64 for the
 // digits, 64 for the output, 16 matrix instructions of 16), a third of what the loads take with all waves of a CU at it.
 #include "fg_attn_common.h"
@@ -56,6 +56,11 @@ struct AttnI8Args {
   float* part_o;               // [b * nh][splits][dh]
 };
 
+template <bool ONCE>
+__device__ __forceinline__ i4_t fetch(const int8_t* p) {
+  const i4_t* q = reinterpret_cast<const i4_t*>(p);
+  return ONCE ? __builtin_nontemporal_load(q) : *q;
+}
 __device__ __forceinline__ int seq_of(const AttnI8Args& a, int row) {
   const int sid = a.seq_ids ? a.seq_ids[row] : row;
   return sid < 0 ? 0 : (sid >= a.n_seqs ? a.n_seqs - 1 : sid);
@@ -73,7 +78,8 @@ __device__ __forceinline__ float quad_sum(float v) {
   return v + dpp_f32<kDppXor2>(v);
 }
 
-template <int DH, int WPU, bool SHARED>
+// ONCE: the pages are loaded as data that is not needed again (see plan_i8).
+template <int DH, int WPU, bool SHARED, bool ONCE>
 __global__ __launch_bounds__(256, 3) void attn_decode_i8_kernel(AttnI8Args a) {
   constexpr int KS = DH / 64;   // steps of 64 over the head size
   constexpr int ND = DH / 16;   // blocks of 16 output rows
@@ -147,12 +153,12 @@ __global__ __launch_bounds__(256, 3) void attn_decode_i8_kernel(AttnI8Args a) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int k = 0; k < KS; ++k) kreg[i][k] = *reinterpret_cast<const i4_t*>(p + 4 * i * DH + 64 * k);
+      for (int k = 0; k < KS; ++k) kreg[i][k] = fetch<ONCE>(p + 4 * i * DH + 64 * k);
   };
   auto load_v = [&](int page) {
     const int8_t* p = a.v_codes + ((int64_t)page * a.nkv + kv) * page_bytes + v_at;
 #pragma unroll
-    for (int j = 0; j < ND; ++j) vreg[j] = *reinterpret_cast<const i4_t*>(p + 256 * j);
+    for (int j = 0; j < ND; ++j) vreg[j] = fetch<ONCE>(p + 256 * j);
   };
 
   const int b_lo = 4 * chunk / per_kv, nb = min(nq - 1, 4 * chunk + 3) / per_kv - b_lo + 1;   // beams of this unit
@@ -376,20 +382,28 @@ __global__ __launch_bounds__(256) void attn_merge_i8_kernel(AttnI8Args a) {
 
 struct Plan {
   int chunks, wpu, splits;
+  bool once;
   int64_t units;
 };
 size_t part_bytes(int64_t rows_heads, int splits, int dh) { return splits > 1 ? align_up((size_t)rows_heads * splits * (dh + 2) * 4, 256) : 0; }
 
 // Waves per unit, and workgroups that share a sequence.  Only the device knows the lengths; what the table could hold stands for
-// them.  Measured, us with 1 / 2 / 4 waves a unit, pages of 64 rows at head size 128:
+// them.  Measured, us with 1 / 2 / 4 waves a unit, pages of 64 rows at head size 128 (ordinary loads):
 //   6144 units, 2 pages 39 / 43 / 54         2048 units, 2 pages 14.4 / 17.6 / 19.5, 7 pages 42.7 / 44.0 / 44.8,
 //   2048 units of 1 to 32 pages (table of 32) 115 / 107 / 104       1536 units of four beams, 8 shared pages 60.9 / 58.3 / 59.6
+//   (57 / 51 / 54 loaded as below)
 //   768 units of four beams, head size 64, 9 pages 19.2 / 18.4 / 18.0    128 units, 32 pages 39.5 / 23.3 / 15.0
 //   1024 units, four to a cache head (their waves meet in the L1 if they share a workgroup) 46.8 / 50.8 / 81.2
 // and where units are few, with 1 / 2 / 4 / 8 / 16 / 32 splits of four waves:
 //   128 units, 32 pages 15.0 / 17.0 / 16.7 / 19.2    32 units, 24 pages 17.1 / 16.4 / 15.4 / 14.6, 125 pages 39.6 / 25.4 / 17.7 / 16.8 /
 //   16.5 / 19.0    8 units, 512 pages 144 / 77 / 43 / 26 / 17.7 / 17.4
-Plan plan_i8(int32_t nh, int32_t nkv, int32_t beams, int32_t b, int32_t table_stride) {
+// Pages that one wave alone reads are loaded as data that is not needed again, where the call reads more than the last-level cache
+// keeps until the next step; us, with the ordinary loads first: 16 x 4 beams, 96 heads, 252 MB 57.9 / 51.0; 64 sequences of 542
+// rows, 96 heads, 870 MB 152 / 138 (6.3 TB/s).  Below that a program's next step may find the pages there: 4 sequences of 2000 rows,
+// 32 heads, 66 MB, repeated 15.0 / 20.0.  The price: 64 sequences that share 512 rows by fours without saying so 87 / 113; the call
+// with beams is for those.  And where several tiles of queries read a cache head's pages the L1 has to keep them:
+// 32 x 4 beams, 32 heads on 8 46 / 60.
+Plan plan_i8(int32_t nh, int32_t nkv, int32_t beams, int32_t b, int32_t dh, int32_t table_stride) {
   Plan p;
   p.chunks = (int)ceil_div(nh / nkv * beams, 4);
   p.units = (int64_t)(b / beams) * nkv * p.chunks;
@@ -399,6 +413,7 @@ Plan plan_i8(int32_t nh, int32_t nkv, int32_t beams, int32_t b, int32_t table_st
     p.wpu = 1;
   else
     p.wpu = 2;
+  p.once = p.chunks == 1 && (double)p.units * table_stride * (2 * FG_PAGE_ROWS * dh) > 128 << 20;
   p.splits = 1;
   if (p.units <= 64 && table_stride >= 24) {   // two pages a wave at least
     const int64_t want = 512 / p.units, most = table_stride / 8;
@@ -411,7 +426,7 @@ Plan plan_i8(int32_t nh, int32_t nkv, int32_t beams, int32_t b, int32_t table_st
 }  // namespace
 
 size_t decode_attention_i8_workspace(int32_t nh, int32_t nkv, int32_t beams, int32_t b, int32_t dh, int32_t table_stride) {
-  const Plan p = plan_i8(nh, nkv, beams, b, table_stride);
+  const Plan p = plan_i8(nh, nkv, beams, b, dh, table_stride);
   return part_bytes((int64_t)b * nh, p.splits, dh) + 256;
 }
 
@@ -420,7 +435,7 @@ int decode_attention_i8_launch(const fg_model_cfg& cfg, int32_t nkv, int32_t bea
                                size_t ws_bytes, hipStream_t stream) {
   if (b == 0) return FG_OK;
   const int dh = cfg.h1 / cfg.nh;
-  Plan p = plan_i8(cfg.nh, nkv, beams, b, seqs.table_stride);
+  Plan p = plan_i8(cfg.nh, nkv, beams, b, dh, seqs.table_stride);
   const int64_t rh = (int64_t)b * cfg.nh;
   if (rh > 0x7fffffff || ceil_div(p.units * p.wpu, 4) > kMostBlocks) return FG_ERR_SHAPE;
   while (p.splits > 1 && (!ws || ws_bytes < part_bytes(rh, p.splits, dh))) p.splits = ws ? p.splits - 1 : 1;
@@ -451,12 +466,16 @@ int decode_attention_i8_launch(const fg_model_cfg& cfg, int32_t nkv, int32_t bea
   const dim3 grid((unsigned)ceil_div(p.units * p.wpu, 4), (unsigned)p.splits);
   const bool shared = beams > 1 && cfg.nh / nkv % 4 != 0;   // else a unit has queries of one row only
   ProfScope prof(FG_K_ATTN_DECODE, stream);
-#define FG_I8_SH(DH_, WPU_)                                                                              \
-  do {                                                                                                   \
-    if (shared)                                                                                          \
-      hipLaunchKernelGGL((attn_decode_i8_kernel<DH_, WPU_, true>), grid, dim3(256), 0, stream, a);       \
-    else                                                                                                 \
-      hipLaunchKernelGGL((attn_decode_i8_kernel<DH_, WPU_, false>), grid, dim3(256), 0, stream, a);      \
+#define FG_I8_LAUNCH(DH_, WPU_, SH_)                                                                        \
+  do {                                                                                                      \
+    if (p.once)                                                                                             \
+      hipLaunchKernelGGL((attn_decode_i8_kernel<DH_, WPU_, SH_, true>), grid, dim3(256), 0, stream, a);     \
+    else                                                                                                    \
+      hipLaunchKernelGGL((attn_decode_i8_kernel<DH_, WPU_, SH_, false>), grid, dim3(256), 0, stream, a);    \
+  } while (0)
+#define FG_I8_SH(DH_, WPU_)                                                                     \
+  do {                                                                                          \
+    if (shared) FG_I8_LAUNCH(DH_, WPU_, true); else FG_I8_LAUNCH(DH_, WPU_, false);             \
   } while (0)
 #define FG_I8(DH_)                                                                                              \
   do {                                                                                                          \
@@ -465,6 +484,7 @@ int decode_attention_i8_launch(const fg_model_cfg& cfg, int32_t nkv, int32_t bea
   if (dh == 128) FG_I8(128); else FG_I8(64);
 #undef FG_I8
 #undef FG_I8_SH
+#undef FG_I8_LAUNCH
   FG_LAUNCH_CHECK();
   if (p.splits > 1) {
     if (dh == 128)

@@ -263,6 +263,27 @@ def test_attention_of_many_pages(nh, nkv, b, beams, n, ws):
         _check_attention(plain, table[i:i + 1], q[i:i + 1], [n], nh, nkv, dh, got[i:i + 1])
 
 
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("nh,b,beams,stride", [(12, 16, 1, 100), (8, 64, 4, 150), (33, 32, 1, 40), (1, 4100, 1, 2), (1, 4100, 1, 5)])
+def test_attention_with_room_for_much(nh, b, beams, stride, dh):
+    """Tables that could hold more pages than a last-level cache, whose sequences are short (head size 64, 4100
+    units with two pages: ones that it could keep): 1, 2 and 4 waves a unit."""
+    lens = [(0, 1, 63, 64, 100, 128)[i % 6] for i in range(b)]
+    plain = P.I8Pages(40, nh, dh, seed=stride)
+    table = np.full((b, stride), -1, np.int32)
+    r = np.random.default_rng(nh)
+    for g in range(0, b, beams):
+        table[g:g + beams, :2] = r.integers(0, plain.n, 2)
+        table[g + beams - 1, 1] = r.integers(0, plain.n)
+    q = _rows((b, nh * dh), 3)
+    cfg = _cfg(nh, dh)
+    pages = _upload(plain, cfg)
+    seqs = B.Ragged(dev(table), None, dev(np.array(lens, np.int32)))
+    got = host(B.fg_decode_attention_beams_paged(cfg, nh, beams, dev(q), nh * dh, b, pages, seqs))
+    some = sorted(set(range(min(b, 12))) | {b // 2, b - 1})
+    _check_attention(plain, table[some], q[some], [lens[i] for i in some], nh, nh, dh, got[some])
+
+
 def test_pages_beyond_32_bits():
     """Codes whose offsets pass 2^32: stored, read back, copied and attended to."""
     nh, dh, cfg = 32, 128, _cfg(32, 128)
