@@ -418,7 +418,7 @@ int64_t fg_diagonal_pages_needed(int32_t n_seqs, int32_t s, int32_t n, int32_t g
  * fg_beam_select (up to 65535 rows, vocab < 2^28): of all continuations (beam j, word w) of a sequence, worth
  *   v = scores[j] + logits[j][w] - log(sum over w' of exp(logits[j][w'])),
  * the n_best (1 .. FG_MAX_BEST) of the largest v, in descending order; among equal ones the larger logit, then the
- * lowest j * vocab + w comes first.  v is compared in binary64 and returned in binary32.
+ * lowest j * vocab + w comes first (-0 equals 0).  v is compared in binary64 and returned in binary32.
  * logits: binary32 rows of cfg->vocab words, row_stride >= vocab elements apart (what fg_lm_head_greedy leaves).
  * A logit of -inf or NaN is no continuation (a forbidden word), +inf counts as the largest binary32 number; scores of
  * -inf or NaN take the beam out.  done (int32 per row, NULL: none): a beam with done != 0 offers itself once, as word

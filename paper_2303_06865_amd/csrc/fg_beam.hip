@@ -27,16 +27,16 @@ constexpr int kList = 512;
 // A forbidden word is -inf (also NaN); +inf counts as the largest finite number.
 __device__ __forceinline__ float clean(float x) { return x >= -FLT_MAX ? fminf(x, FLT_MAX) : -INFINITY; }
 
-// order-preserving bits: larger number, larger key
+// order-preserving bits: larger number, larger key (-0 is 0)
 __device__ __forceinline__ uint32_t ordered(float x) {
-  const uint32_t u = __builtin_bit_cast(uint32_t, x);
+  const uint32_t u = __builtin_bit_cast(uint32_t, x + 0.f);
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 __device__ __forceinline__ float from_ordered(uint32_t u) {
   return __builtin_bit_cast(float, u & 0x80000000u ? u & 0x7fffffffu : ~u);
 }
 __device__ __forceinline__ uint64_t ordered(double x) {
-  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  const uint64_t u = __builtin_bit_cast(uint64_t, x + 0.0);
   return u >> 63 ? ~u : u | (1ull << 63);
 }
 

@@ -78,6 +78,16 @@ def test_select_ties_and_forbidden_words():
     _check_select(x, np.zeros(8, np.float32), 4, 32, np.ones(8, np.int32), eos=0)
 
 
+def test_select_zeros_of_both_signs_are_equal():
+    """-0 is 0: the lowest word wins among them, and the lowest beam among scores of -0 and 0."""
+    x = np.zeros((4, 3000), np.float32)
+    x[:, ::3] = -0.0
+    x[:, 1500:] = -4.0
+    for beams, best in ((1, 32), (2, 7), (4, 32)):
+        _check_select(x, np.zeros(4, np.float32), beams, best)
+    _check_select(x, np.array([-0.0, 0.0, -0.0, 0.0], np.float32), 4, 4, np.ones(4, np.int32), eos=5)
+
+
 def test_select_where_the_best_lie_together():
     """The best words next to each other, at the ends, and a whole row in ascending or descending order."""
     vocab = 50272
