@@ -31,6 +31,7 @@ namespace fg {
 namespace {
 
 typedef int i4_t __attribute__((ext_vector_type(4)));
+typedef uint16_t us8_t __attribute__((ext_vector_type(8)));
 
 constexpr float kWeightTop = 268435392.0f;
 constexpr float kQueryTop = 133160000.0f;                             // off by two roundings: 133160016 at most
@@ -110,17 +111,22 @@ __global__ __launch_bounds__(256, 3) void attn_decode_i8_kernel(AttnI8Args a) {
   {
     const half_t* src = a.q + (int64_t)row * a.q_stride + (int64_t)head * DH + 16 * g;
     h8_t x[KS][2];
-    float top = 0.f;
+    // Magnitudes are ordered as their bits.  An infinity or a NaN in the query makes top infinite, so every score a NaN, so the
+    // output too.
+    us8_t bits = (us8_t)(uint16_t)0;
 #pragma unroll
     for (int k = 0; k < KS; ++k)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         x[k][h] = *reinterpret_cast<const h8_t*>(src + 64 * k + 8 * h);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf((float)x[k][h][e]));
+        bits = __builtin_elementwise_max(__builtin_bit_cast(us8_t, x[k][h]) & (us8_t)(uint16_t)0x7fff, bits);
       }
+    uint16_t most = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) most = bits[e] > most ? bits[e] : most;
+    float top = most >= 0x7c00 ? INFINITY : (float)__builtin_bit_cast(half_t, most);
     top = xor32_reduce(xor16_reduce(top, OpMax()), OpMax());
-    const float inv = top > 0.f ? kQueryTop / top : 0.f;
+    const float inv = top > 0.f && top < INFINITY ? kQueryTop / top : 0.f;
 #pragma unroll
     for (int k = 0; k < KS; ++k)
 #pragma unroll
@@ -133,7 +139,7 @@ __global__ __launch_bounds__(256, 3) void attn_decode_i8_kernel(AttnI8Args a) {
         qop[k][w] = (int)(y | (y & 0x40404040u) << 1);
       }
     // scores come out in log2 units; the digit's weight goes in here
-    qmul = top * (a.scale * kLog2e / kQueryTop) * (float)(1 << (7 * dig));
+    qmul = top < INFINITY ? top * (a.scale * kLog2e / kQueryTop) * (float)(1 << (7 * dig)) : NAN;
   }
   const int n_of = qi < nq ? n_row : 0x7fffffff;   // an idle column is never masked, and never written
   const int n_max = __builtin_amdgcn_readfirstlane((int)wave_max((float)((n_row + 63) >> 6)));   // pages: exact in binary32
@@ -277,7 +283,7 @@ __global__ __launch_bounds__(256, 3) void attn_decode_i8_kernel(AttnI8Args a) {
 #pragma unroll
         for (int j = 0; j < ND; ++j) o[j] *= alpha;
       }
-      const float bv = beta * vs;
+      const float bv = beta > 0.f ? beta * vs : 0.f;   // a page that is not this beam's may hold infinities
 #pragma unroll
       for (int j = 0; j < ND; ++j) {
         const i4_t z = {0, 0, 0, 0};
@@ -299,7 +305,7 @@ __global__ __launch_bounds__(256, 3) void attn_decode_i8_kernel(AttnI8Args a) {
     for (int r = 0; r < 4; ++r) o[j][r] = quad_sum(o[j][r] * wd);
   if (WPU == 1 && a.splits == 1) {
     if (qi < nq && there) {
-      const float inv = l > 0.f ? 1.0f / l : 0.f;   // no rows attended: zeros
+      const float inv = l == 0.f ? 0.f : 1.0f / l;   // no rows attended: zeros
       half_t* dst = a.out + ((int64_t)row * a.nh + head) * DH + 4 * g;
 #pragma unroll
       for (int j = 0; j < ND; ++j)
@@ -339,7 +345,7 @@ __global__ __launch_bounds__(256, 3) void attn_decode_i8_kernel(AttnI8Args a) {
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
       if (a.splits == 1)
-        a.out[rh * DH + lane + 64 * k] = (half_t)(den > 0.f ? num[k] / den : 0.f);
+        a.out[rh * DH + lane + 64 * k] = (half_t)(den == 0.f ? 0.f : num[k] / den);
       else
         a.part_o[(rh * a.splits + split) * DH + lane + 64 * k] = num[k];
     }
@@ -377,7 +383,7 @@ __global__ __launch_bounds__(256) void attn_merge_i8_kernel(AttnI8Args a) {
   for (int k = 0; k < N; ++k) sm[wave][lane + 64 * k] = num[k];
   __syncthreads();
   const int d = threadIdx.x;
-  if (d < DH) a.out[rh * DH + d] = (half_t)(den > 0.f ? (sm[0][d] + sm[1][d] + sm[2][d] + sm[3][d]) / den : 0.f);
+  if (d < DH) a.out[rh * DH + d] = (half_t)(den == 0.f ? 0.f : (sm[0][d] + sm[1][d] + sm[2][d] + sm[3][d]) / den);
 }
 
 struct Plan {

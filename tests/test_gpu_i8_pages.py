@@ -341,6 +341,39 @@ def test_attention_extremes():
     _check_attention(plain, table, q, lens, nh, nh, dh, host(got))
 
 
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("b,beams,n", [(4, 4, 100), (4, 1, 100), (4, 2, 3000), (1200, 2, 70)])
+def test_attention_keeps_infinities_to_whom_they_belong(dh, b, beams, n):
+    """A query with an infinity or a NaN gives NaN; a page whose scale is one gives NaN to the beams that read it, with nothing
+    of it in the other queries' results: those are the same bits as without it."""
+    nh, cfg = 2, _cfg(2, dh)
+    lens = [n] * b
+    plain, table, q = _attend_case(nh, nh, dh, lens, beams, n - 40, seed=b)
+    own = table[1, (n - 1) // 64]
+    assert (table == own).sum() == 1                        # the last page of row 1 is its own
+    seqs = B.Ragged(dev(table), None, dev(np.array(lens, np.int32)))
+    run = lambda p, x: host(B.fg_decode_attention_beams_paged(cfg, nh, beams, dev(x), x.shape[1], b, p, seqs)).reshape(b, nh, dh)
+    pages = _upload(plain, cfg)
+    good = run(pages, q)
+    assert np.isfinite(good).all()
+    for value in (np.inf, -np.inf, np.nan):
+        odd = q.copy()
+        odd[2, dh + dh // 2 + 1] = value                    # row 2, head 1
+        got = run(pages, odd)
+        assert np.isnan(got[2, 1]).all()
+        got[2, 1] = good[2, 1]
+        assert np.array_equal(got, good)
+    for scales in (pages.k_meta, pages.v_meta):
+        for value in (np.inf, np.nan):
+            was = float(scales[own, 0])
+            scales[own, 0] = value
+            got = run(pages, q)
+            scales[own, 0] = was
+            assert not np.isfinite(got[1, 0]).any()
+            got[1, 0] = good[1, 0]
+            assert np.array_equal(got, good)
+
+
 def test_calls_on_another_stream():
     nh, dh, cfg = 3, 64, _cfg(3, 64)
     plain = P.I8Pages(4, nh, dh)
