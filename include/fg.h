@@ -123,6 +123,8 @@ typedef struct {
  * positions of one head dimension lie next to each other: the order in which the matrix cores contract over
  * positions); k_meta/v_meta [n_pages][nh] binary32 scales (4-byte aligned).
  * Their contents do not matter before a page's first position is stored.
+ * A row with an infinity or NaN makes the scale of its page and head infinite: all of that page and head is NaN then, until
+ * its first position is stored again; other pages and heads are not touched.
  * In the other formats rows are stored exactly as in fg_kv_cache; only their place differs. */
 #define FG_PAGE_ROWS 64
 typedef struct {

@@ -68,7 +68,9 @@ __device__ __forceinline__ us8_t abs_max(const h8_t v, us8_t top) {
 __device__ __forceinline__ float largest(us8_t t) {
   const uint16_t a = __builtin_elementwise_max(__builtin_elementwise_max(t[0], t[1]), __builtin_elementwise_max(t[2], t[3]));
   const uint16_t b = __builtin_elementwise_max(__builtin_elementwise_max(t[4], t[5]), __builtin_elementwise_max(t[6], t[7]));
-  return (float)__builtin_bit_cast(half_t, (uint16_t)__builtin_elementwise_max(a, b));
+  // (a NaN, above infinity by its bits, counts as one: a maximum of numbers would lose it, and with it what it hides)
+  const uint16_t most = __builtin_elementwise_max(a, b), inf = 0x7c00;
+  return (float)__builtin_bit_cast(half_t, (uint16_t)__builtin_elementwise_min(most, inf));
 }
 
 __device__ __forceinline__ u2_t row_codes(const h8_t x, const Step& s) {

@@ -116,6 +116,38 @@ def test_append_leaves_everything_else():
     _same(pages, plain)
 
 
+@pytest.mark.parametrize("nh,dh", [(3, 128), (5, 64)])
+@pytest.mark.parametrize("s,at", [(1, 10), (1, 0), (70, 10)])
+@pytest.mark.parametrize("value", [np.inf, -np.inf, np.nan])
+def test_append_of_infinities_and_nan(nh, dh, s, at, value):
+    """The page and head that gets one is NaN as a whole, and stays so for rows stored behind it; all others are as without it.
+    Storing the page's first position again makes it a page like any other."""
+    cfg, h1 = _cfg(nh, dh), nh * dh
+    good, odd = B.KVPages(cfg, 3, int8=True), B.KVPages(cfg, 3, int8=True)
+    table = dev(np.array([[2, 0, 1]], np.int32))
+    put = lambda p, k, v, pos: B.fg_kv_append_paged(cfg, dev(k), dev(v), h1, 1, k.shape[0], p, B.Ragged(table, None, dev(np.array([pos], np.int32))))
+    first, rows, behind = _rows((2, 64, h1), 1), _rows((2, s, h1), 2, 3.0), _rows((2, 1, h1), 3)
+    bad = rows.copy()
+    bad[0, s - 1, dh + 3], bad[1, s - 1, dh + 9] = value, value      # head 1, the last row
+    page = (at + s - 1) // 64
+    for p, x in ((good, rows), (odd, bad)):
+        if at:
+            put(p, first[0, :at], first[1, :at], 0)
+        put(p, x[0], x[1], at)
+        put(p, behind[0], behind[1], at + s)
+    n = at + s + 1
+    read = lambda p: [host(t).reshape(n, nh, dh) for t in B.fg_kv_gather_paged(cfg, p, B.Ragged(table), 1, n)]
+    for a, b in zip(read(good), read(odd)):
+        assert np.isfinite(a).all()
+        assert np.isnan(b[64 * page:, 1]).all()
+        b[64 * page:, 1] = a[64 * page:, 1]
+        assert np.array_equal(a, b)
+    for p in (good, odd):
+        put(p, first[0], first[1], 64 * page)
+    for a, b in zip(read(good), read(odd)):
+        assert np.array_equal(a, b)
+
+
 @pytest.mark.parametrize("fmt", ["i8", "f16", "q4", "q4h"])
 @pytest.mark.parametrize("nh,dh,s", [(3, 128, 1), (5, 64, 77), (2, 128, 130), (8, 64, 64)])
 def test_gather_reads_rows_back(fmt, nh, dh, s):
