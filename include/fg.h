@@ -441,8 +441,9 @@ size_t fg_beam_select_workspace_bytes(const fg_model_cfg* cfg, int32_t n_groups,
  * beams that were chosen: row i takes over the state of row parents[i] of its group (0 .. beams-1; anything else: its
  * own), i.e. table_out[i] = table_in[parent], pos_out[i] = pos_in[parent] (rows cached), entries past the pages held are -1.
  * Full pages are shared, not copied.  The page where row i's next position goes (slot pos/64) becomes row i's alone:
- * if it is partly filled, the first row of the group that holds it keeps it and the others take a free page and a copy
- * of its filled rows (up to the next multiple of 16) in every layer; if it is not begun, every row takes a free page.
+ * if it is partly filled, the first row of the group that has it there keeps it, unless a row of the group (of greater
+ * length) holds it as a full page; the others take a free page and a copy of its filled rows (up to the next multiple
+ * of 16) in every layer; if it is not begun, every row takes a free page.
  * Group g owns pages g*pages_per_group .. (g+1)*pages_per_group - 1 of the pools (all below n_pages); free are those
  * that no row of the group holds any more, and the lowest is taken first (so nobody else may hold pages of that range).  Pages outside the group's range (a prompt
  * shared between groups) are only read: a row whose partly filled page lies there takes a copy.  A row that finds no

@@ -371,7 +371,8 @@ struct ReorderArgs {
 };
 
 // One workgroup per group.  A thread takes a column of the group's table: it reads the entries of all beams before it
-// writes any, so the table may be rewritten in place.  Pages held are marked in a bitmap in LDS.  24 groups of 4: 5.3 us, latency.
+// writes any, so the table may be rewritten in place.  Pages held are marked in a bitmap in LDS: the full ones first, so that a
+// begun page that somebody holds as a full one is known, then the begun ones.  24 groups of 4: 5.3 us, latency.
 __global__ __launch_bounds__(256) void beam_table_kernel(ReorderArgs a) {
   extern __shared__ uint32_t held[];   // one bit per page of the group
   __shared__ int parent[FG_MAX_BEAMS], raw[FG_MAX_BEAMS], last[FG_MAX_BEAMS];
@@ -401,8 +402,10 @@ __global__ __launch_bounds__(256) void beam_table_kernel(ReorderArgs a) {
         for (int k = 0; k < a.beams; ++k) pg = k == parent[j] ? e[k] : pg;
       a.table_out[(row0 + j) * a.stride + c] = pg;
       const int loc = pg - first;
-      if (pg >= first && loc < a.per_group) atomicOr(&held[loc >> 5], 1u << (loc & 31));
-      if (c == n >> 6) last[j] = pg;   // the page begun, or -1
+      if (c == n >> 6)
+        last[j] = pg;   // the page begun, or -1
+      else if (pg >= first && loc < a.per_group)
+        atomicOr(&held[loc >> 5], 1u << (loc & 31));
     }
   }
   __syncthreads();
@@ -411,8 +414,13 @@ __global__ __launch_bounds__(256) void beam_table_kernel(ReorderArgs a) {
   const int n = tid < a.beams ? rows_of(tid) : 0, slot = n >> 6;
   const bool begun = (n & 63) != 0, fits = tid < a.beams && slot < a.stride;
   const int was = tid < a.beams ? last[tid] : -1;
-  bool keeps = begun && was >= first && was - first < a.per_group;
+  const bool owned = begun && was >= first && was - first < a.per_group;
+  const uint32_t bit = owned ? 1u << ((was - first) & 31) : 0u;
+  bool keeps = owned && !(held[(was - first) >> 5] & bit);
   for (int k = 0; k < a.beams; ++k) keeps = keeps && !(k < tid && last[k] == was && (rows_of(k) & 63) != 0);
+  wave_lds_fence();   // all lanes have seen the full pages alone
+  if (owned) atomicOr(&held[(was - first) >> 5], bit);
+  wave_lds_fence();
   const bool takes = fits && !keeps;
   const uint64_t takers = __builtin_amdgcn_ballot_w64(takes);
   const int rank = __builtin_popcountll(takers & ((1ull << tid) - 1)), need = __builtin_popcountll(takers);
