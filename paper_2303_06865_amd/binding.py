@@ -574,11 +574,13 @@ def beam_select_workspace(cfg: Cfg, n_groups: int, beams: int, n_best: int) -> t
 
 def fg_beam_select(cfg: Cfg, logits: torch.Tensor, scores: torch.Tensor, beams: int, n_best: Optional[int] = None,
                    done: Optional[torch.Tensor] = None, eos: int = -1, ws: Optional[torch.Tensor] = None, inplace: bool = False):
-    """logits float32 [n * beams, vocab] (rows may be apart), scores float32 [n * beams], done int32 [n * beams] or None.
+    """logits float32 [n * beams, vocab] (rows may be apart, but not overlap), scores float32 [n * beams], done int32 [n * beams] or None.
     Returns (beams int32, ids int32, scores float32, done int32), each [n, n_best], best first; inplace (n_best == beams): the
     last two are written over scores and done."""
     rows, vocab = logits.shape
     assert logits.dtype == torch.float32 and logits.stride(1) == 1 and vocab == cfg.vocab
+    row_stride = logits.stride(0) if rows > 1 else vocab
+    assert row_stride >= vocab, "rows of logits have to be vocab elements apart at least (one row for several beams: repeat it)"
     assert scores.dtype == torch.float32 and scores.is_contiguous() and scores.numel() == rows
     assert done is None or (done.dtype == torch.int32 and done.is_contiguous() and done.numel() == rows)
     assert rows % beams == 0
@@ -592,8 +594,8 @@ def fg_beam_select(cfg: Cfg, logits: torch.Tensor, scores: torch.Tensor, beams: 
         out, out_done = scores.view(n, beams), out_done if done is None else done.view(n, beams)
     if ws is None:
         ws = beam_select_workspace(cfg, n, beams, n_best)
-    _check(lib().fg_beam_select(C.byref(cfg.c), n, beams, n_best, _p(logits), max(logits.stride(0), cfg.vocab), _p(scores),
-                                _p(done), eos, _p(out_beams), _p(ids), _p(out), _p(out_done), _p(ws), ws.numel(), _stream(device)),
+    _check(lib().fg_beam_select(C.byref(cfg.c), n, beams, n_best, _p(logits), row_stride, _p(scores), _p(done), eos,
+                                _p(out_beams), _p(ids), _p(out), _p(out_done), _p(ws), ws.numel(), _stream(device)),
            "fg_beam_select")
     return out_beams, ids, out, out_done
 
