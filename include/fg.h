@@ -340,8 +340,9 @@ int fg_decode_attention_paged(const fg_model_cfg* cfg, const void* q_f16, int64_
  * beams: rows i*beams .. i*beams + beams-1 (b % beams == 0, beams <= FG_MAX_BEAMS) are expected to share pages, as
  * the beams of one sequence share those of its prompt: a page that several of them name for the same positions is
  * read once.  Results do not depend on `beams`, up to the order of sums; any mixture of shared and own pages is right.
- * A query (row and head) with an infinity or NaN, or with a page of its own rows whose scale is one, gives NaN or infinities, and
- * no other query's result is touched by it; rows without positions give zeros.
+ * A query (row and head) with an infinity or NaN, or with a page of its own rows whose scale is one, gives NaN or
+ * infinities (also where that page's weight is too small for a number), and no other query's result is touched by it;
+ * rows without positions give zeros.
  * ws (FG_ERR_WORKSPACE without it) holds the partial results of long sequences that are split over workgroups; sized
  * for b rows and tables of table_stride pages; one ws serves one call at a time.  The other calls on 8-bit pages (fg_decode_attention_paged, the paged
  * layers, fg_generate_diagonal) run the same kernel with beams = 1, nkv = nh; fg_decode_attention_paged, which has no

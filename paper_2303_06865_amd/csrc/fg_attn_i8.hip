@@ -240,7 +240,8 @@ __global__ __launch_bounds__(256, 3) void attn_decode_i8_kernel(AttnI8Args a) {
       __builtin_amdgcn_sched_barrier(0);
       if (v + 1 < count) load_k(page_n);
       __builtin_amdgcn_sched_barrier(0);
-      const float f = qmul * ks;
+      // a scale of infinity: NaN, whatever the signs and the weights (digit sums of one sign would give -inf, a weight of 0)
+      const float f = ks < INFINITY ? qmul * ks : NAN;
       float s[4][4];
 #pragma unroll
       for (int i = 0; i < 4; ++i)
@@ -283,7 +284,8 @@ __global__ __launch_bounds__(256, 3) void attn_decode_i8_kernel(AttnI8Args a) {
 #pragma unroll
         for (int j = 0; j < ND; ++j) o[j] *= alpha;
       }
-      const float bv = beta > 0.f ? beta * vs : 0.f;   // a page that is not this beam's may hold infinities
+      // a page that is not this beam's may hold infinities; one that is keeps them, also where its weight underflows
+      const float bv = top == -INFINITY ? 0.f : beta * vs;
 #pragma unroll
       for (int j = 0; j < ND; ++j) {
         const i4_t z = {0, 0, 0, 0};
