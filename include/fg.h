@@ -121,7 +121,8 @@ typedef struct {
  * k_codes/v_codes [n_pages][nh][64][dh] halves, metas NULL.
  * FG_I8P64 pages: k_codes [n_pages][nh][64][dh] bytes; v_codes [n_pages][nh][4][dh][16] bytes (16 consecutive
  * positions of one head dimension lie next to each other: the order in which the matrix cores contract over
- * positions); k_meta/v_meta [n_pages][nh] binary32 scales (4-byte aligned).
+ * positions); k_meta/v_meta [n_pages][nh] binary32 scales (4-byte aligned).  A value is scale * code, codes are
+ * -127 .. 127.
  * Their contents do not matter before a page's first position is stored.
  * A row with an infinity or NaN makes the scale of its page and head infinite: all of that page and head is NaN then, until
  * its first position is stored again; other pages and heads are not touched.

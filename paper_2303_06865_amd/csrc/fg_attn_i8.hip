@@ -2,11 +2,12 @@
 // heads on the same keys and values at once.
 //
 // Both products run on the integer matrix cores, on the stored codes as they are: no code is ever unpacked.  What stands on
-// the other side is a number in four digits of seven bits:
-//   q_d = (max |q| / Cq) * sum_t 2^(7t) a_td,   -64 <= a_td <= 63,   Cq = 133160000: +-Cq fit into such digits
-//   p_j =             1 / Cp * sum_t 2^(7t) b_tj,    0 <= b_tj <= 127,   Cp = 2^28 - 64     (p = 2^(s - max over the page) <= 1)
-// so that q.k = (max|q| / Cq) S_k sum_t 2^(7t) (a_t . c) with exact 32-bit integer sums, put together in binary32.  Queries are
-// off by 2^-26 of their largest element, weights by 2^-28 of the page's largest: below what binary32 sums lose.  The four
+// the other side is a number in four digits:
+//   q_d = 2^(E - 30) (sum_t 2^(8t) a_td + r_d / 1024),   -128 <= a_td <= 127,   2^E > max |q|,   |r_d| < 1024
+//   p_j =     1 / Cp * sum_t 2^(7t) b_tj,    0 <= b_tj <= 127,   Cp = 2^28 - 64     (p = 2^(s - max over the page) <= 1)
+// so that q.k = 2^(E - 30) S_k sum_t 2^(8t) (a_t . c) with exact 32-bit integer sums, put together in binary32.  Queries are exact
+// like that: up to a magnitude of 64, 2^(E - 30) is no larger than FP16's smallest step; beyond it the rests r, whole numbers of two
+// more digits, are multiplied where one is not zero.  Weights are off by 2^-28 of the page's largest.  The four
 // digits are four columns of v_mfma_i32_16x16x64_i8; its sixteen columns are four queries: the beams of a sequence that share
 // the page, or the query heads of a cache head, or (one query) idle, at no cost, because the loads are what bounds this.
 //
@@ -34,8 +35,7 @@ typedef int i4_t __attribute__((ext_vector_type(4)));
 typedef uint16_t us8_t __attribute__((ext_vector_type(8)));
 
 constexpr float kWeightTop = 268435392.0f;
-constexpr float kQueryTop = 133160000.0f;                             // off by two roundings: 133160016 at most
-constexpr int kQueryShift = 64 * (1 + 128 + 16384 + 2097152);         // digits from 0: kQueryShift + 133160895 = 2^28 - 1
+constexpr int kQueryBits = 30;   // (2^31 does not fit into such digits)
 
 struct AttnI8Args {
   const half_t* q;
@@ -79,6 +79,16 @@ __device__ __forceinline__ float quad_sum(float v) {
   return v + dpp_f32<kDppXor2>(v);
 }
 
+// The lane's digit of four whole numbers below 2^31 - 2^23, one a byte: with 128 (of each digit) added, digits are from 0.
+// which: 0x0c0c0400 + 0x0101 * digit.
+__device__ __forceinline__ int digits4(const float (&n)[4], uint32_t which) {
+  uint32_t u[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) u[e] = (uint32_t)(int)n[e] + 0x80808080u;
+  const uint32_t lo = __builtin_amdgcn_perm(u[1], u[0], which), hi = __builtin_amdgcn_perm(u[3], u[2], which);
+  return (int)(__builtin_amdgcn_perm(hi, lo, 0x05040100u) ^ 0x80808080u);
+}
+
 // ONCE: the pages are loaded as data that is not needed again (see plan_i8).
 template <int DH, int WPU, bool SHARED, bool ONCE>
 __global__ __launch_bounds__(256, 3) void attn_decode_i8_kernel(AttnI8Args a) {
@@ -108,6 +118,8 @@ __global__ __launch_bounds__(256, 3) void attn_decode_i8_kernel(AttnI8Args a) {
   const int n_row = rows_of(a, row);
   i4_t qop[KS];
   float qmul;
+  bool fine;   // some query of the wave has rests
+  i4_t* rests = reinterpret_cast<i4_t*>(&sm_o[wave][0][0]);   // as many bytes as the wave's outputs take later
   {
     const half_t* src = a.q + (int64_t)row * a.q_stride + (int64_t)head * DH + 16 * g;
     h8_t x[KS][2];
@@ -126,20 +138,42 @@ __global__ __launch_bounds__(256, 3) void attn_decode_i8_kernel(AttnI8Args a) {
     for (int e = 0; e < 8; ++e) most = bits[e] > most ? bits[e] : most;
     float top = most >= 0x7c00 ? INFINITY : (float)__builtin_bit_cast(half_t, most);
     top = xor32_reduce(xor16_reduce(top, OpMax()), OpMax());
-    const float inv = top > 0.f && top < INFINITY ? kQueryTop / top : 0.f;
+    // 2^E > top and all its powers: E is -23 .. 16.  (top 0 or infinite: elements are 0 or do not matter)
+    const bool any = top > 0.f && top < INFINITY;
+    const int e2 = any ? (int)(__builtin_bit_cast(uint32_t, top) >> 23) - 126 : 0;
+    const float up = any ? __builtin_bit_cast(float, (uint32_t)(127 + kQueryBits - e2) << 23) : 0.f;
+    const uint32_t which = 0x0c0c0400u + 0x0101u * dig;
 #pragma unroll
     for (int k = 0; k < KS; ++k)
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
-        uint32_t d[4];
+        float n[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          d[e] = ((uint32_t)((int)((float)x[k][w >> 1][4 * (w & 1) + e] * inv) + kQueryShift) >> (7 * dig)) & 127u;
-        const uint32_t y = (d[0] | d[1] << 8 | d[2] << 16 | d[3] << 24) ^ 0x40404040u;   // less 64, in eight bits
-        qop[k][w] = (int)(y | (y & 0x40404040u) << 1);
+        for (int e = 0; e < 4; ++e) n[e] = (float)x[k][w >> 1][4 * (w & 1) + e] * up;   // exact; whole but for the rests
+        qop[k][w] = digits4(n, which);
       }
     // scores come out in log2 units; the digit's weight goes in here
-    qmul = top < INFINITY ? top * (a.scale * kLog2e / kQueryTop) * (float)(1 << (7 * dig)) : NAN;
+    qmul = top < INFINITY ? a.scale * kLog2e * __builtin_bit_cast(float, (uint32_t)(127 + e2 - kQueryBits + 8 * dig) << 23) : NAN;
+    fine = __builtin_amdgcn_ballot_w64(e2 > kQueryBits - 24) != 0;   // FP16 has no step below 2^-24
+    if (__builtin_expect(fine, 0)) {   // (a loop, the elements loaded again: little code, seldom run)
+      uint32_t odd = 0;
+#pragma unroll 1
+      for (int i = 0; i < 4 * KS; ++i) {
+        const h4_t z = *reinterpret_cast<const h4_t*>(src + 64 * (i >> 2) + 4 * (i & 3));
+        float n[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float y = (float)z[e] * up;
+          n[e] = (y - __builtin_truncf(y)) * 1024.f;   // whole
+        }
+        const uint32_t d = (uint32_t)digits4(n, which);
+        reinterpret_cast<uint32_t*>(rests + 64 * (i >> 2) + lane)[i & 3] = d;   // (read by this lane only)
+        odd |= d;
+      }
+      fine = __builtin_amdgcn_ballot_w64(odd != 0) != 0;
+      if (fine) qmul *= 1.0f / 1024;
+      wave_lds_fence();
+    }
   }
   const int n_of = qi < nq ? n_row : 0x7fffffff;   // an idle column is never masked, and never written
   const int n_max = __builtin_amdgcn_readfirstlane((int)wave_max((float)((n_row + 63) >> 6)));   // pages: exact in binary32
@@ -237,6 +271,16 @@ __global__ __launch_bounds__(256, 3) void attn_decode_i8_kernel(AttnI8Args a) {
 #pragma unroll
         for (int k = 0; k < KS; ++k) acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(kreg[i][k], qop[k], acc[i], 0, 0, 0);
       }
+      if (__builtin_expect(fine, 0)) {   // in 32 bits still: 128 products of 127 * 128, 1025 times, are below 2^31
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i] *= 1024;
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+          const i4_t rest = rests[64 * k + lane];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(kreg[i][k], rest, acc[i], 0, 0, 0);
+        }
+      }
       __builtin_amdgcn_sched_barrier(0);
       if (v + 1 < count) load_k(page_n);
       __builtin_amdgcn_sched_barrier(0);
@@ -299,6 +343,7 @@ __global__ __launch_bounds__(256, 3) void attn_decode_i8_kernel(AttnI8Args a) {
   }
 
   // ---- digits together, then waves, then (second launch) splits
+  wave_lds_fence();   // the rests have been read
   const float wd = (float)(1 << (7 * dig)) / kWeightTop;
   const float l = xor32_reduce(xor16_reduce(l_run, OpAdd()), OpAdd());
 #pragma unroll

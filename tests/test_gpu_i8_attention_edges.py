@@ -1,5 +1,5 @@
-"""Attention over 8-bit pages where a page's scale is an infinity, and where few sequences of any length lie in long tables (split
-over workgroups), against binary64.
+"""Attention over 8-bit pages where elements of a query differ by many orders of magnitude, where a page's scale is an infinity,
+and where few sequences of any length lie in long tables (split over workgroups), against binary64.
 
 Tolerance.  Codes and queries enter the products exactly, as integer sums per digit of the query; the score is f times the sum of
 four such numbers (f: the query's and the page's scales).  The digits of a number have magnitudes that add up to at most 3.02 times
@@ -48,6 +48,47 @@ def _run(cfg, nh, nkv, dh, beams, q, table, lens, pages, **kw):
 def _close(got, want, tol):
     err = np.abs(got.astype(np.float64) - want)
     assert (err <= tol).all(), float((err / np.maximum(tol, 1e-30)).max())
+
+
+@pytest.mark.parametrize("nh,nkv,dh,beams,b,n", [(2, 2, 128, 1, 2, 100), (2, 2, 64, 2, 4, 3000), (4, 1, 128, 1, 1, 3000), (6, 1, 64, 4, 4, 200),
+                                                 (2, 2, 128, 4, 4, 70), (1, 1, 128, 1, 1100, 70), (1, 1, 64, 1, 2100, 70)])
+@pytest.mark.parametrize("top", [1.0, 63.0, 70.0, 200.0, 2000.0, 60000.0])
+def test_queries_with_one_large_element(nh, nkv, dh, beams, b, n, top):
+    """The large element meets keys of zero; the scores are those of the others, down to subnormal ones."""
+    lens = [n] * b
+    stride = -(-n // 64)
+    shared = min(b, 8)
+    plain = P.I8Pages(shared * stride, nkv, dh, seed=int(top))
+    table = np.tile(_table(shared, stride, plain.n, 1), (-(-b // shared), 1))[:b]
+    table = np.repeat(table[::beams], beams, 0)
+    r = np.random.default_rng(b)
+    at = r.integers(0, dh)
+    plain.codes[0][:, :, :, at] = 0
+    plain.scales[0] *= 40
+    plain.scales[1][:] = 2.0 ** -6
+    q = _rows((b, nh * dh), 3)
+    x = q.reshape(b, nh, dh)
+    x[:, :, ::3] *= np.float16(2.0 ** -7)
+    x[:, :, 1::5] *= np.float16(2.0 ** -14)
+    x[:, :, at] = top
+    x[::2, :, at] *= -1
+    got = _run(_cfg(nh, dh), nh, nkv, dh, beams, q, table, lens, _upload(plain, B.Cfg(nkv * dh, nkv, 64, 64, 64)))
+    some = sorted(set(range(min(b, 9))) | {b - 1})
+    _close(got[some], *_exact(plain, table[some], q[some], [n] * len(some), nh, nkv, dh))
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+def test_queries_of_any_magnitude(dh):
+    """All elements of one size, from the smallest subnormal number to the largest number."""
+    nh, n, b = 2, 90, 12
+    plain = P.I8Pages(2 * b, nh, dh, seed=dh)
+    table = _table(b, 2, plain.n, 1)
+    q = np.random.default_rng(5).choice(np.array([-1.0, -0.75, 0.5, 1.0]), (b, nh * dh))
+    q = (q * np.array([2.0 ** -24, 2.0 ** -23, 2.0 ** -16, 2.0 ** -8, 0.3, 1.99, 31.9, 63.97, 64, 127.9, 128, 60000])[:, None]).astype(np.float16)
+    for i in range(b):   # the scores stay where the weights are ordinary
+        plain.scales[0][table[i]] *= np.float32(2.0 / max(1.0, float(np.abs(q[i]).max())))
+    got = _run(_cfg(nh, dh), nh, nh, dh, 1, q, table, [n] * b, _upload(plain, _cfg(nh, dh)))
+    _close(got, *_exact(plain, table, q, [n] * b, nh, nh, dh))
 
 
 @pytest.mark.parametrize("dh", [64, 128])
