@@ -344,11 +344,11 @@ int fg_decode_attention_paged(const fg_model_cfg* cfg, const void* q_f16, int64_
  * A query (row and head) with an infinity or NaN, or with a page of its own rows whose scale is one, gives NaN or
  * infinities (also where that page's weight is too small for a number), and no other query's result is touched by it;
  * rows without positions give zeros.
- * ws (FG_ERR_WORKSPACE without it) holds the partial results of long sequences that are split over workgroups; sized
- * for b rows and tables of table_stride pages; one ws serves one call at a time.  The other calls on 8-bit pages (fg_decode_attention_paged, the paged
+ * ws (FG_ERR_WORKSPACE without it) holds the partial results of long sequences that are split over workgroups; the
+ * size for b rows and tables of table_stride pages is enough for fewer rows and shorter tables too (same cfg, nkv and
+ * beams); one ws serves one call at a time.  The other calls on 8-bit pages (fg_decode_attention_paged, the paged
  * layers, fg_generate_diagonal) run the same kernel with beams = 1, nkv = nh; fg_decode_attention_paged, which has no
- * workspace, never splits a sequence (for a few long sequences this call is the faster one), the layers split as far as
- * their own workspace reaches. */
+ * workspace, never splits a sequence (for a few long sequences this call is the faster one), the layers use theirs. */
 #define FG_MAX_BEAMS 16
 int fg_decode_attention_beams_paged(const fg_model_cfg* cfg, int32_t nkv, int32_t beams, const void* q_f16,
                                     int64_t q_row_stride, int32_t b, const fg_kv_pages* pages, const fg_ragged* seqs,
@@ -432,7 +432,8 @@ int64_t fg_diagonal_pages_needed(int32_t n_seqs, int32_t s, int32_t n, int32_t g
  * Outputs, [n_groups][n_best]: the beam 0 .. beams-1 continued, the word, its v, and (NULL: not wanted) out_done =
  * done of the beam, or word == eos (eos < 0: never).  Where there are fewer continuations than n_best, the rest are
  * beam -1, word -1, v = -inf, done 1.  With n_best == beams, out_scores may be scores and out_done may be done (a search that
- * keeps its state in place); no other overlaps.  ws >= fg_beam_select_workspace_bytes; one ws serves one call at a time. */
+ * keeps its state in place); no other overlaps.  ws >= fg_beam_select_workspace_bytes, whose size is enough for fewer
+ * sequences, beams and n_best of the same cfg too; one ws serves one call at a time. */
 #define FG_MAX_BEST 32
 int fg_beam_select(const fg_model_cfg* cfg, int32_t n_groups, int32_t beams, int32_t n_best, const float* logits,
                    int64_t row_stride, const float* scores, const int32_t* done, int32_t eos, int32_t* out_beams,

@@ -433,6 +433,7 @@ __global__ __launch_bounds__(256) void attn_merge_i8_kernel(AttnI8Args a) {
   if (d < DH) a.out[rh * DH + d] = (half_t)(den == 0.f ? 0.f : (sm[0][d] + sm[1][d] + sm[2][d] + sm[3][d]) / den);
 }
 
+constexpr int kMostSplitUnits = 64;
 struct Plan {
   int chunks, wpu, splits;
   bool once;
@@ -468,7 +469,7 @@ Plan plan_i8(int32_t nh, int32_t nkv, int32_t beams, int32_t b, int32_t dh, int3
     p.wpu = 2;
   p.once = p.chunks == 1 && (double)p.units * table_stride * (2 * FG_PAGE_ROWS * dh) > 128 << 20;
   p.splits = 1;
-  if (p.units <= 64 && table_stride >= 24) {   // two pages a wave at least
+  if (p.units <= kMostSplitUnits && table_stride >= 24) {   // two pages a wave at least
     const int64_t want = 512 / p.units, most = table_stride / 8;
     p.splits = (int)(want < most ? want : most);
     if (p.splits > kMostSplits) p.splits = kMostSplits;
@@ -479,8 +480,7 @@ Plan plan_i8(int32_t nh, int32_t nkv, int32_t beams, int32_t b, int32_t dh, int3
 }  // namespace
 
 size_t decode_attention_i8_workspace(int32_t nh, int32_t nkv, int32_t beams, int32_t b, int32_t dh, int32_t table_stride) {
-  const Plan p = plan_i8(nh, nkv, beams, b, dh, table_stride);
-  return part_bytes((int64_t)b * nh, p.splits, dh) + 256;
+  return part_bytes((int64_t)b * nh, plan_i8(nh, nkv, beams, b, dh, table_stride).splits, dh) + 256;
 }
 
 int decode_attention_i8_launch(const fg_model_cfg& cfg, int32_t nkv, int32_t beams, const half_t* q, int64_t q_stride, int32_t b,
@@ -491,7 +491,7 @@ int decode_attention_i8_launch(const fg_model_cfg& cfg, int32_t nkv, int32_t bea
   Plan p = plan_i8(cfg.nh, nkv, beams, b, dh, seqs.table_stride);
   const int64_t rh = (int64_t)b * cfg.nh;
   if (rh > 0x7fffffff || ceil_div(p.units * p.wpu, 4) > kMostBlocks) return FG_ERR_SHAPE;
-  while (p.splits > 1 && (!ws || ws_bytes < part_bytes(rh, p.splits, dh))) p.splits = ws ? p.splits - 1 : 1;
+  if (p.splits > 1 && (!ws || ws_bytes < part_bytes(rh, p.splits, dh))) p.splits = 1;
   AttnI8Args a;
   a.q = q;
   a.q_stride = q_stride;
@@ -560,7 +560,14 @@ static bool beams_ok(const fg_model_cfg* cfg, int32_t nkv, int32_t beams, int32_
 extern "C" size_t fg_decode_attention_beams_workspace_bytes(const fg_model_cfg* cfg, int32_t nkv, int32_t beams, int32_t b,
                                                             int32_t table_stride) {
   if (!cfg || check_cfg(cfg) || !beams_ok(cfg, nkv, beams, b) || b == 0 || table_stride <= 0) return 0;
-  return decode_attention_i8_workspace(cfg->nh, nkv, beams, b, cfg->h1 / cfg->nh, table_stride);
+  // few rows are split over more workgroups and can need more than many: what the largest of the smaller batches needs
+  size_t most = 0;
+  for (int32_t n = beams; n <= b; n += beams) {
+    const size_t need = decode_attention_i8_workspace(cfg->nh, nkv, beams, n, cfg->h1 / cfg->nh, table_stride);
+    most = need > most ? need : most;
+    if (n / beams >= kMostSplitUnits) break;   // no larger batch is split
+  }
+  return most;
 }
 
 extern "C" int fg_decode_attention_beams_paged(const fg_model_cfg* cfg, int32_t nkv, int32_t beams, const void* q_f16,

@@ -513,9 +513,10 @@ __global__ __launch_bounds__(256) void beam_copy_kernel(CopyArgs a) {
 struct SelectPlan {
   int vpt, pieces, piece;
 };
+constexpr int kFullChip = 512;
 SelectPlan plan_select(int64_t rows, int vocab) {
   SelectPlan p;
-  p.vpt = rows * ceil_div(vocab, 8192) >= 512 ? 32 : 8;
+  p.vpt = rows * ceil_div(vocab, 8192) >= kFullChip ? 32 : 8;
   p.pieces = (int)ceil_div(vocab, 256 * p.vpt);
   p.piece = (int)align_up((size_t)ceil_div(vocab, p.pieces), 4);   // even: every group of threads has words
   p.pieces = (int)ceil_div(vocab, p.piece);
@@ -560,7 +561,11 @@ extern "C" size_t fg_beam_select_workspace_bytes(const fg_model_cfg* cfg, int32_
   if (!cfg || check_cfg(cfg) || !groups_ok(n_groups, beams) || n_groups == 0 || n_best < 1 || n_best > FG_MAX_BEST) return 0;
   if (cfg->vocab > (int)kMostWord || (int64_t)n_groups * beams > 65535) return 0;
   const int64_t rows = (int64_t)n_groups * beams;
-  return carve_select_ws(rows, plan_select(rows, cfg->vocab), n_best, nullptr).total;
+  // the most rows in small pieces can need more than more rows in large ones: enough for any smaller call as well
+  const int64_t most_small = (kFullChip - 1) / ceil_div(cfg->vocab, 8192), small = rows < most_small ? rows : most_small;
+  const size_t need = carve_select_ws(rows, plan_select(rows, cfg->vocab), n_best, nullptr).total;
+  const size_t of_small = small > 0 ? carve_select_ws(small, plan_select(small, cfg->vocab), n_best, nullptr).total : 0;
+  return need > of_small ? need : of_small;
 }
 
 extern "C" int fg_beam_select(const fg_model_cfg* cfg, int32_t n_groups, int32_t beams, int32_t n_best, const float* logits,

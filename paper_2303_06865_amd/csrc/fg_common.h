@@ -144,7 +144,7 @@ int decode_attention_paged_launch(const fg_model_cfg& cfg, const half_t* q, int6
                                   hipStream_t stream);
 int check_pages(const fg_model_cfg* cfg, const fg_kv_pages* pages, const fg_ragged* seqs);
 // 8-bit pages (csrc/fg_kv_i8.hip, csrc/fg_attn_i8.hip): rows b of `beams` that share pages, nkv cache heads; without a
-// workspace, or with less than decode_attention_i8_workspace, sequences are split over fewer workgroups
+// workspace, or with less than decode_attention_i8_workspace (for this call alone), sequences are not split
 int kv_append_i8_launch(const fg_model_cfg& cfg, const half_t* k, const half_t* v, int64_t row_stride, int32_t b, int32_t s,
                         const fg_kv_pages& pages, const fg_ragged& seqs, bool use_pos, hipStream_t stream);
 size_t decode_attention_i8_workspace(int32_t nh, int32_t nkv, int32_t beams, int32_t b, int32_t dh, int32_t table_stride);
