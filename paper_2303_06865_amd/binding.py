@@ -318,7 +318,7 @@ class KVPages:
         int8: 8-bit codes (FG_I8P64), keys [n_pages, nh, 64, dh], values [n_pages, nh, 4, dh, 16] (16 positions of
         one head dimension next to each other), one binary32 scale per page and head [n_pages, nh]."""
         self.n_pages, self.meta_f16, self.quantized = n_pages, bool(meta_f16 and quantized and not int8), quantized
-        self.int8 = int8
+        self.int8, self.nh, self.dh = int8, cfg.nh, cfg.dh
         mk = torch.zeros if zero else torch.empty
         nh, dh = cfg.nh, cfg.dh
         if int8:
@@ -326,37 +326,52 @@ class KVPages:
             self.v_codes = mk((n_pages, nh, PAGE_ROWS // 16, dh, 16), dtype=torch.int8, device=device)
             self.k_meta = mk((n_pages, nh), dtype=torch.float32, device=device)
             self.v_meta = mk((n_pages, nh), dtype=torch.float32, device=device)
-            self.c = fg_kv_pages(_p(self.k_codes), _p(self.k_meta), _p(self.v_codes), _p(self.v_meta), FG_I8P64, n_pages)
+            self._finish(FG_I8P64)
             return
         if not quantized:
             self.k_codes = mk((n_pages, nh, PAGE_ROWS, dh), dtype=torch.float16, device=device)
             self.v_codes = mk((n_pages, nh, PAGE_ROWS, dh), dtype=torch.float16, device=device)
             self.k_meta = self.v_meta = None
-            self.c = fg_kv_pages(_p(self.k_codes), None, _p(self.v_codes), None, FG_F16, n_pages)
+            self._finish(FG_F16)
             return
         mt = torch.float16 if meta_f16 else torch.float32
         self.k_codes = mk((n_pages, nh, PAGE_ROWS, dh // 2), dtype=torch.uint8, device=device)
         self.v_codes = mk((n_pages, nh, PAGE_ROWS, dh // 2), dtype=torch.uint8, device=device)
         self.k_meta = mk((n_pages, nh, PAGE_ROWS, dh // 64, 2), dtype=mt, device=device)
         self.v_meta = mk((n_pages, nh, PAGE_ROWS, dh // 64, 2), dtype=mt, device=device)
-        self.c = fg_kv_pages(_p(self.k_codes), _p(self.k_meta), _p(self.v_codes), _p(self.v_meta),
-                             FG_Q4G64_H16 if meta_f16 else FG_Q4G64, n_pages)
+        self._finish(FG_Q4G64_H16 if meta_f16 else FG_Q4G64)
 
     @staticmethod
     def of(k_codes: torch.Tensor, k_meta: Optional[torch.Tensor], v_codes: torch.Tensor, v_meta: Optional[torch.Tensor],
            dtype: int) -> "KVPages":
         """A pool over tensors that the caller made, in the shapes above (e.g. one layer of a tensor that holds all)."""
+        assert dtype in (FG_F16, FG_Q4G64, FG_Q4G64_H16, FG_I8P64), "not a format of pages"
+        f16, int8 = dtype == FG_F16, dtype == FG_I8P64
+        n, nh = k_codes.shape[:2]
+        dh = k_codes.shape[-1] * (1 if f16 or int8 else 2)
+        rows = (n, nh, PAGE_ROWS, k_codes.shape[-1])
+        assert k_codes.shape == rows and v_codes.shape == ((n, nh, PAGE_ROWS // 16, dh, 16) if int8 else rows), \
+            "shape of the codes"
+        assert k_codes.dtype == v_codes.dtype == (torch.float16 if f16 else torch.int8 if int8 else torch.uint8), "type of the codes"
+        for m in (k_meta, v_meta):
+            assert (m is None) == f16, "all formats but FP16 have metas"
+            assert f16 or m.shape == ((n, nh) if int8 else (n, nh, PAGE_ROWS, dh // 64, 2)), "shape of the metas"
+            assert f16 or m.dtype == (torch.float16 if dtype == FG_Q4G64_H16 else torch.float32), "type of the metas"
         for t in (k_codes, k_meta, v_codes, v_meta):
-            assert t is None or (t.is_cuda and t.is_contiguous() and t.shape[:2] == k_codes.shape[:2])
-        assert k_codes.numel() == v_codes.numel() and k_codes.dtype == v_codes.dtype
-        assert k_codes.dtype == {FG_F16: torch.float16, FG_I8P64: torch.int8}.get(dtype, torch.uint8)
-        assert (k_meta is None) == (v_meta is None) == (dtype == FG_F16)
-        assert k_meta is None or k_meta.dtype == v_meta.dtype == (torch.float16 if dtype == FG_Q4G64_H16 else torch.float32)
+            assert t is None or (t.is_cuda and t.is_contiguous() and t.device == k_codes.device)
         p = KVPages.__new__(KVPages)
-        p.n_pages, p.meta_f16, p.quantized, p.int8 = k_codes.shape[0], dtype == FG_Q4G64_H16, dtype != FG_F16, dtype == FG_I8P64
+        p.n_pages, p.meta_f16, p.quantized, p.int8, p.nh, p.dh = n, dtype == FG_Q4G64_H16, not f16, int8, nh, dh
         p.k_codes, p.k_meta, p.v_codes, p.v_meta = k_codes, k_meta, v_codes, v_meta
-        p.c = fg_kv_pages(_p(k_codes), _p(k_meta), _p(v_codes), _p(v_meta), dtype, p.n_pages)
+        p._finish(dtype)
         return p
+
+    def _finish(self, dtype: int) -> None:
+        self.c = fg_kv_pages(_p(self.k_codes), _p(self.k_meta), _p(self.v_codes), _p(self.v_meta), dtype, self.n_pages)
+        self.kind = (self.nh, self.dh, self.k_codes.get_device())   # what the C calls cannot see
+
+    def check(self, nh: int, dh: int) -> None:
+        """The kernels take the pool's heads and head size from the call's configuration."""
+        assert self.nh == nh and self.dh == dh, "pages of %d heads of %d in a call of %d heads of %d" % (self.nh, self.dh, nh, dh)
 
     def nbytes(self) -> int:
         n = 2 * self.k_codes.numel() * self.k_codes.element_size()
@@ -370,9 +385,14 @@ class Ragged:
     def __init__(self, page_table: torch.Tensor, seq_ids: Optional[torch.Tensor] = None,
                  pos: Optional[torch.Tensor] = None):
         for t in (page_table, seq_ids, pos):
-            assert t is None or (t.dtype == torch.int32 and t.is_cuda and t.is_contiguous())
+            assert t is None or (t.dtype == torch.int32 and t.is_cuda and t.is_contiguous() and t.device == page_table.device)
         self.page_table, self.seq_ids, self.pos = page_table, seq_ids, pos
         self.c = fg_ragged(_p(page_table), _p(seq_ids), _p(pos), page_table.shape[1], page_table.shape[0])
+
+    def check(self, b: int) -> None:
+        """The kernels read b entries."""
+        assert (self.pos is None or self.pos.numel() >= b) and (self.seq_ids is None or self.seq_ids.numel() >= b), \
+            "pos and seq_ids have to name all %d rows" % b
 
 
 def _ws(nbytes: int, device="cuda") -> Optional[torch.Tensor]:
@@ -513,12 +533,14 @@ def fg_decode_layer(cfg: Cfg, w: LayerWeights, x: torch.Tensor, t: int, kv: KVCa
 
 def fg_kv_append_paged(cfg: Cfg, k: torch.Tensor, v: torch.Tensor, row_stride: int, b: int, s: int, pages: KVPages,
                        seqs: Ragged) -> None:
+    pages.check(cfg.nh, cfg.dh)
     _check(lib().fg_kv_append_paged(C.byref(cfg.c), _p(k), _p(v), row_stride, b, s, C.byref(pages.c), C.byref(seqs.c),
                                     _stream()), "fg_kv_append_paged")
 
 
 def fg_decode_attention_paged(cfg: Cfg, q: torch.Tensor, q_row_stride: int, b: int, pages: KVPages, seqs: Ragged,
                               rows_bias: int = 0) -> torch.Tensor:
+    pages.check(cfg.nh, cfg.dh)
     out = torch.empty((b, cfg.h1), dtype=torch.float16, device=q.device)
     _check(lib().fg_decode_attention_paged(C.byref(cfg.c), _p(q), q_row_stride, b, C.byref(pages.c), C.byref(seqs.c),
                                            rows_bias, _p(out), _stream()), "fg_decode_attention_paged")
@@ -533,6 +555,16 @@ def _on_this_device(*tensors: Optional[torch.Tensor]) -> int:
     return dev
 
 
+def _check_rows(t: torch.Tensor, rows: int, row_stride: int, cols: int, what: str) -> None:
+    """t is FP16 and holds `rows` rows of `cols` elements, row_stride elements apart from its first one on (columns of a wider
+    tensor, mostly: what lies behind them in the last row belongs to it)."""
+    assert t.dtype == torch.float16, what + " has to be FP16"
+    if t.dim() == 2 and t.stride(0) == row_stride and t.shape[0] >= rows and t.shape[1] >= cols and t.stride(1) == 1:
+        return
+    room = t.untyped_storage().nbytes() // 2 - t.storage_offset()
+    assert rows == 0 or (rows - 1) * row_stride + cols <= room, "%s is smaller than %d rows, %d elements apart" % (what, rows, row_stride)
+
+
 def decode_attention_beams_workspace(cfg: Cfg, nkv: int, beams: int, b: int, table_stride: int) -> torch.Tensor:
     return _ws(lib().fg_decode_attention_beams_workspace_bytes(C.byref(cfg.c), nkv, beams, b, table_stride))
 
@@ -541,8 +573,12 @@ def fg_decode_attention_beams_paged(cfg: Cfg, nkv: int, beams: int, q: torch.Ten
                                     pages: KVPages, seqs: Ragged, rows_bias: int = 0, ws: Optional[torch.Tensor] = None,
                                     out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Attention of b rows over 8-bit pages of nkv heads; each `beams` rows in turn share the pages that their tables share."""
-    assert q.dtype == torch.float16 and pages.k_codes.shape[1] == nkv
-    device = _on_this_device(q, out, ws, pages.k_codes)
+    pages.check(nkv, cfg.dh)
+    seqs.check(b)
+    _check_rows(q, b, q_row_stride, cfg.h1, "q")
+    if out is not None:
+        _check_rows(out, b, cfg.h1, cfg.h1, "out")
+    device = _on_this_device(q, out, ws, pages.k_codes, seqs.page_table)
     if out is None:
         out = torch.empty((b, cfg.h1), dtype=torch.float16, device=q.device)
     if ws is None:
@@ -555,14 +591,21 @@ def fg_decode_attention_beams_paged(cfg: Cfg, nkv: int, beams: int, q: torch.Ten
 
 def fg_kv_gather_paged(cfg: Cfg, pages: KVPages, seqs: Ragged, b: int, s: int, k_out: Optional[torch.Tensor] = None,
                        v_out: Optional[torch.Tensor] = None, row_stride: Optional[int] = None):
-    """Positions pos[i] .. pos[i] + s - 1 of sequence seq_ids[i] as FP16 (k, v), [b, s, h1]."""
-    assert pages.k_codes.shape[1] == cfg.nh
-    device = _on_this_device(pages.k_codes, k_out, v_out)
-    assert k_out is None or k_out.dtype == v_out.dtype == torch.float16
+    """Positions pos[i] .. pos[i] + s - 1 of sequence seq_ids[i] as FP16 (k, v), [b, s, h1]; with tensors of the caller's, rows
+    row_stride elements apart (h1 if not given)."""
+    pages.check(cfg.nh, cfg.dh)
+    seqs.check(b)
+    assert (k_out is None) == (v_out is None), "k_out and v_out: both or none"
     if k_out is None:
+        assert row_stride is None, "row_stride belongs to the caller's tensors"
         k_out = torch.empty((b, s, cfg.h1), dtype=torch.float16, device=pages.k_codes.device)
         v_out = torch.empty_like(k_out)
         row_stride = cfg.h1
+    else:
+        row_stride = cfg.h1 if row_stride is None else row_stride
+        _check_rows(k_out, b * s, row_stride, cfg.h1, "k_out")
+        _check_rows(v_out, b * s, row_stride, cfg.h1, "v_out")
+    device = _on_this_device(pages.k_codes, seqs.page_table, k_out, v_out)
     _check(lib().fg_kv_gather_paged(C.byref(cfg.c), C.byref(pages.c), C.byref(seqs.c), b, s, _p(k_out), _p(v_out),
                                     row_stride, _stream(device)), "fg_kv_gather_paged")
     return k_out, v_out
@@ -614,11 +657,15 @@ def fg_beam_reorder_paged(cfg: Cfg, pages: Sequence[KVPages], table: torch.Tenso
     for t in (table, pos, parents, table_out, pos_out, missing):
         assert t is None or (t.dtype == torch.int32 and t.is_contiguous())
     assert pos.numel() == rows and parents.numel() == rows and rows % beams == 0
-    assert pages[0].k_codes.shape[1] == cfg.nh
+    pages[0].check(cfg.nh, cfg.dh)
     device = _on_this_device(table, pos, parents, table_out, pos_out, missing, ws, pages[0].k_codes)
+    kind = pages[0].kind
+    for p in pages:
+        assert p.kind == kind, "the layers' pools have to be of one kind, on one device"
     table_out = torch.empty_like(table) if table_out is None else table_out
     pos_out = torch.empty_like(pos) if pos_out is None else pos_out
     assert table_out.shape == table.shape and pos_out.numel() == rows
+    assert missing is None or missing.numel() >= rows // beams
     if missing is None:
         missing = torch.empty((rows // beams,), dtype=torch.int32, device=table.device)
     if ws is None:
@@ -645,6 +692,7 @@ def fg_decode_layer_paged(cfg: Cfg, w: LayerWeights, x: torch.Tensor, pages: KVP
                           ws: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
                           topk: int = 0, beams: int = 1) -> torch.Tensor:
     """beams > 1 (fg_decode_layer_beams_paged): each `beams` rows in turn are expected to share pages; no topk."""
+    pages.check(cfg.nh, cfg.dh)
     x = _f16(x)
     b = x.shape[0]
     if out is None:
@@ -664,6 +712,7 @@ def fg_decode_layer_paged(cfg: Cfg, w: LayerWeights, x: torch.Tensor, pages: KVP
 
 def fg_prefill_layer_paged(cfg: Cfg, w: LayerWeights, x: torch.Tensor, pages: KVPages, seqs: Ragged,
                            ws: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    pages.check(cfg.nh, cfg.dh)
     x = _f16(x)
     b, s, _ = x.shape
     if out is None:
@@ -729,6 +778,8 @@ def fg_generate_diagonal(cfg: Cfg, layers: Sequence[LayerWeights], embed: torch.
     n_seqs, s = prompt.shape
     l = len(layers)
     larr = (fg_layer_weights * l)(*[w.c for w in layers])
+    for p in pages:
+        p.check(cfg.nh, cfg.dh)
     parr = (fg_kv_pages * l)(*[p.c for p in pages])
     if out_ids is None:
         out_ids = torch.zeros((n_seqs, n), dtype=torch.int32, device=prompt.device)
