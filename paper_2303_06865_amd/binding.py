@@ -367,7 +367,8 @@ class KVPages:
 
     def _finish(self, dtype: int) -> None:
         self.c = fg_kv_pages(_p(self.k_codes), _p(self.k_meta), _p(self.v_codes), _p(self.v_meta), dtype, self.n_pages)
-        self.kind = (self.nh, self.dh, self.k_codes.get_device())   # what the C calls cannot see
+        self.device = self.k_codes.get_device()
+        self.kind = (self.nh, self.dh, self.device)   # what the C calls cannot see
 
     def check(self, nh: int, dh: int) -> None:
         """The kernels take the pool's heads and head size from the call's configuration."""
@@ -387,12 +388,13 @@ class Ragged:
         for t in (page_table, seq_ids, pos):
             assert t is None or (t.dtype == torch.int32 and t.is_cuda and t.is_contiguous() and t.device == page_table.device)
         self.page_table, self.seq_ids, self.pos = page_table, seq_ids, pos
+        self.device = page_table.get_device()
+        self.rows = min(t.numel() if t is not None else 0x7fffffff for t in (seq_ids, pos))   # a call's rows at most
         self.c = fg_ragged(_p(page_table), _p(seq_ids), _p(pos), page_table.shape[1], page_table.shape[0])
 
     def check(self, b: int) -> None:
         """The kernels read b entries."""
-        assert (self.pos is None or self.pos.numel() >= b) and (self.seq_ids is None or self.seq_ids.numel() >= b), \
-            "pos and seq_ids have to name all %d rows" % b
+        assert self.rows >= b, "pos and seq_ids have to name all %d rows" % b
 
 
 def _ws(nbytes: int, device="cuda") -> Optional[torch.Tensor]:
@@ -559,10 +561,11 @@ def _check_rows(t: torch.Tensor, rows: int, row_stride: int, cols: int, what: st
     """t is FP16 and holds `rows` rows of `cols` elements, row_stride elements apart from its first one on (columns of a wider
     tensor, mostly: what lies behind them in the last row belongs to it)."""
     assert t.dtype == torch.float16, what + " has to be FP16"
-    if t.dim() == 2 and t.stride(0) == row_stride and t.shape[0] >= rows and t.shape[1] >= cols and t.stride(1) == 1:
+    need = (rows - 1) * row_stride + cols if rows else 0
+    if t.is_contiguous() and t.numel() >= need:
         return
     room = t.untyped_storage().nbytes() // 2 - t.storage_offset()
-    assert rows == 0 or (rows - 1) * row_stride + cols <= room, "%s is smaller than %d rows, %d elements apart" % (what, rows, row_stride)
+    assert need <= room, "%s is smaller than %d rows, %d elements apart" % (what, rows, row_stride)
 
 
 def decode_attention_beams_workspace(cfg: Cfg, nkv: int, beams: int, b: int, table_stride: int) -> torch.Tensor:
@@ -578,7 +581,8 @@ def fg_decode_attention_beams_paged(cfg: Cfg, nkv: int, beams: int, q: torch.Ten
     _check_rows(q, b, q_row_stride, cfg.h1, "q")
     if out is not None:
         _check_rows(out, b, cfg.h1, cfg.h1, "out")
-    device = _on_this_device(q, out, ws, pages.k_codes, seqs.page_table)
+    device = _on_this_device(q, out, ws)
+    assert pages.device == seqs.device == device, "pages and tables have to be on the current device"
     if out is None:
         out = torch.empty((b, cfg.h1), dtype=torch.float16, device=q.device)
     if ws is None:
@@ -605,7 +609,8 @@ def fg_kv_gather_paged(cfg: Cfg, pages: KVPages, seqs: Ragged, b: int, s: int, k
         row_stride = cfg.h1 if row_stride is None else row_stride
         _check_rows(k_out, b * s, row_stride, cfg.h1, "k_out")
         _check_rows(v_out, b * s, row_stride, cfg.h1, "v_out")
-    device = _on_this_device(pages.k_codes, seqs.page_table, k_out, v_out)
+    device = _on_this_device(k_out, v_out)
+    assert pages.device == seqs.device == device, "pages and tables have to be on the current device"
     _check(lib().fg_kv_gather_paged(C.byref(cfg.c), C.byref(pages.c), C.byref(seqs.c), b, s, _p(k_out), _p(v_out),
                                     row_stride, _stream(device)), "fg_kv_gather_paged")
     return k_out, v_out
@@ -658,10 +663,10 @@ def fg_beam_reorder_paged(cfg: Cfg, pages: Sequence[KVPages], table: torch.Tenso
         assert t is None or (t.dtype == torch.int32 and t.is_contiguous())
     assert pos.numel() == rows and parents.numel() == rows and rows % beams == 0
     pages[0].check(cfg.nh, cfg.dh)
-    device = _on_this_device(table, pos, parents, table_out, pos_out, missing, ws, pages[0].k_codes)
-    kind = pages[0].kind
+    device = _on_this_device(table, pos, parents, table_out, pos_out, missing, ws)
+    kind = (cfg.nh, cfg.dh, device)
     for p in pages:
-        assert p.kind == kind, "the layers' pools have to be of one kind, on one device"
+        assert p.kind == kind, "the layers' pools have to be alike, on the current device"
     table_out = torch.empty_like(table) if table_out is None else table_out
     pos_out = torch.empty_like(pos) if pos_out is None else pos_out
     assert table_out.shape == table.shape and pos_out.numel() == rows

@@ -39,8 +39,8 @@ def _pool(nh=4, dh=64, n=8, **kw):
 def _seqs(b, ids=None):
     """What the calls read of a Ragged (which wants device tensors)."""
     s = B.Ragged.__new__(B.Ragged)
-    s.page_table, s.pos = torch.zeros((b, 2), dtype=torch.int32), torch.zeros(b, dtype=torch.int32)
-    s.seq_ids = None if ids is None else torch.zeros(ids, dtype=torch.int32)
+    s.page_table, s.pos, s.device = torch.zeros((b, 2), dtype=torch.int32), torch.zeros(b, dtype=torch.int32), -1
+    s.seq_ids, s.rows = None if ids is None else torch.zeros(ids, dtype=torch.int32), min(b, ids or b)
     s.c = B.fg_ragged(None, None, None, 2, b)
     return s
 
