@@ -62,6 +62,9 @@ template <int CTRL>
 __device__ __forceinline__ Key1 dpp(Key1 a) { return {dpp64<CTRL>(a.k)}; }
 template <int CTRL>
 __device__ __forceinline__ Key2 dpp(Key2 a) { return {dpp64<CTRL>(a.v), dpp64<CTRL>(a.k)}; }
+__device__ __forceinline__ uint64_t lane_xor(uint64_t v, int m) { return __shfl_xor((unsigned long long)v, m, 64); }
+__device__ __forceinline__ Key1 lane_xor(Key1 a, int m) { return {lane_xor(a.k, m)}; }
+__device__ __forceinline__ Key2 lane_xor(Key2 a, int m) { return {lane_xor(a.v, m), lane_xor(a.k, m)}; }
 // in registers: over each 16 lanes by DPP, then over the wave
 template <class Op>
 __device__ __forceinline__ double row16_f64(double v, Op op) {
@@ -154,13 +157,7 @@ __device__ __forceinline__ int block_best(int n, K mine, K* list /* [kList] */, 
     __syncthreads();
     last = tops[tid & 63];
     __syncthreads();   // read before the next round writes
-    for (int m = 1; m < 64; m <<= 1) {
-      K o = last;
-      uint32_t* w = reinterpret_cast<uint32_t*>(&o);
-#pragma unroll
-      for (int i = 0; i < (int)(sizeof(K) / 4); ++i) w[i] = (uint32_t)__shfl_xor((int)w[i], m, 64);
-      last = larger(last, o);
-    }
+    for (int m = 1; m < 64; m <<= 1) last = larger(last, lane_xor(last, m));
     if (tid == 0) emit(p, last);
   }
   return n;
