@@ -124,8 +124,8 @@ typedef struct {
  * positions); k_meta/v_meta [n_pages][nh] binary32 scales (4-byte aligned).  A value is scale * code, codes are
  * -127 .. 127.
  * Their contents do not matter before a page's first position is stored.
- * A row with an infinity or NaN makes the scale of its page and head infinite: all of that page and head is NaN then, until
- * its first position is stored again; other pages and heads are not touched.
+ * A row with an infinity or NaN makes the scale of its page and head infinite: all of that page and head is NaN
+ * then, until its first position is stored again; other pages and heads are not touched.
  * In the other formats rows are stored exactly as in fg_kv_cache; only their place differs. */
 #define FG_PAGE_ROWS 64
 typedef struct {
@@ -320,10 +320,10 @@ size_t fg_workspace_bytes(const fg_model_cfg* cfg, const fg_layer_weights* layer
 /* ---- Appendix, "Diagonal block schedule": paged cache, sequences at different steps --------
  * fg_kv_append_paged: like fg_kv_append, rows [b, s, h1]; row j of sequence i goes to position
  * pos[i] + j of sequence seq_ids[i], through the page table.  FG_I8P64 pages: a sequence that seq_ids names more than
- * once is appended to in the order of the rows i; two DIFFERENT sequences of one call whose tables name the same page
- * for the positions written leave that page's contents undefined (fg_beam_reorder_paged gives every beam a page of
- * its own there).  For attention with fewer cache heads than query heads, pass a cfg of the cache's heads
- * (h1 = nkv * dh, nh = nkv). */
+ * once is appended to in the order of the rows i; two DIFFERENT sequences of one call whose tables name the same
+ * page for the positions written, or one sequence whose table names a page twice there, leave that page's contents
+ * undefined (fg_beam_reorder_paged gives every beam a page of its own there).  For attention with fewer cache heads
+ * than query heads, pass a cfg of the cache's heads (h1 = nkv * dh, nh = nkv). */
 int fg_kv_append_paged(const fg_model_cfg* cfg, const void* k_f16, const void* v_f16, int64_t row_stride,
                        int32_t b, int32_t s, const fg_kv_pages* pages, const fg_ragged* seqs, void* stream);
 
@@ -340,7 +340,8 @@ int fg_decode_attention_paged(const fg_model_cfg* cfg, const void* q_f16, int64_
  * head h / (nh / nkv).
  * beams: rows i*beams .. i*beams + beams-1 (b % beams == 0, beams <= FG_MAX_BEAMS) are expected to share pages, as
  * the beams of one sequence share those of its prompt: a page that several of them name for the same positions is
- * read once.  Results do not depend on `beams`, up to the order of sums; any mixture of shared and own pages is right.
+ * read once for up to four queries (beams times query heads of its cache head), once in four for more.  Results do not
+ * depend on `beams`, up to the order of sums; any mixture of shared and own pages is right.
  * A query (row and head) with an infinity or NaN, or with a page of its own rows whose scale is one, gives NaN or
  * infinities (also where that page's weight is too small for a number), and no other query's result is touched by it;
  * rows without positions give zeros.
@@ -358,7 +359,8 @@ size_t fg_decode_attention_beams_workspace_bytes(const fg_model_cfg* cfg, int32_
 
 /* Rows of a paged cache as FP16, any page format: row j of k_out, v_out [b, s, h1] (consecutive rows row_stride
  * elements apart, a multiple of 8) is what position pos[i] + j of sequence seq_ids[i] holds: its value rounded to
- * binary32 and then to FP16 (seqs->pos NULL: from position 0).  Positions that the table or the pool does not have (see fg_ragged) give zeros. */
+ * binary32 and then to FP16 (seqs->pos NULL: from position 0).  Positions that the table or the pool does not have
+ * (see fg_ragged) give zeros. */
 int fg_kv_gather_paged(const fg_model_cfg* cfg, const fg_kv_pages* pages, const fg_ragged* seqs, int32_t b, int32_t s,
                        void* k_out_f16, void* v_out_f16, int64_t row_stride, void* stream);
 
@@ -377,9 +379,10 @@ int fg_decode_layer_paged(const fg_model_cfg* cfg, const fg_layer_weights* wts, 
                           int32_t topk, const fg_kv_pages* pages, const fg_ragged* seqs, void* x_out, void* ws,
                           size_t ws_bytes, void* stream);
 
-/* fg_decode_layer_paged (topk = 0) for beam search: rows i*beams .. i*beams + beams-1 are expected to share pages, and on 8-bit
- * pages (FG_I8P64) the attention reads a shared page once for all of them (fg_decode_attention_beams_paged); with other formats it
- * is fg_decode_layer_paged.  b % beams == 0, 1 <= beams <= FG_MAX_BEAMS. */
+/* fg_decode_layer_paged (topk = 0) for beam search: rows i*beams .. i*beams + beams-1 are expected to share pages,
+ * and on 8-bit pages (FG_I8P64) the attention reads a shared page once for four of them
+ * (fg_decode_attention_beams_paged); with other formats it is fg_decode_layer_paged.  b % beams == 0,
+ * 1 <= beams <= FG_MAX_BEAMS. */
 int fg_decode_layer_beams_paged(const fg_model_cfg* cfg, const fg_layer_weights* wts, const void* x_in, int32_t b,
                                 int32_t beams, const fg_kv_pages* pages, const fg_ragged* seqs, void* x_out, void* ws,
                                 size_t ws_bytes, void* stream);
@@ -423,17 +426,20 @@ int64_t fg_diagonal_pages_needed(int32_t n_seqs, int32_t s, int32_t n, int32_t g
  *
  * fg_beam_select (up to 65535 rows, vocab < 2^28): of all continuations (beam j, word w) of a sequence, worth
  *   v = scores[j] + logits[j][w] - log(sum over w' of exp(logits[j][w'])),
- * the n_best (1 .. FG_MAX_BEST) of the largest v, in descending order; among equal ones the larger logit, then the
- * lowest j * vocab + w comes first (-0 equals 0).  v is compared in binary64 and returned in binary32.
+ * the n_best (1 .. FG_MAX_BEST) of the largest v, in descending order; among equal ones the larger logit (of a done
+ * beam: 0), then the lowest j * vocab + w comes first (-0 equals 0).  v is put together and compared in binary64 and
+ * returned in binary32; the sum under the logarithm has binary32 exponentials and is off by up to 2^-17 of itself by
+ * its roundings (2^-21 was the most in rows of 5000 to 256000 words).  So the words of one beam are in order, and words
+ * of different beams whose v are closer than that come in either order, the same one in every run.
  * logits: binary32 rows of cfg->vocab words, row_stride >= vocab elements apart (what fg_lm_head_greedy leaves).
  * A logit of -inf or NaN is no continuation (a forbidden word), +inf counts as the largest binary32 number; scores of
  * -inf or NaN take the beam out.  done (int32 per row, NULL: none): a beam with done != 0 offers itself once, as word
  * `eos` (0 <= eos < vocab, else FG_ERR_SHAPE) at its own score, and its logits do not matter.
  * Outputs, [n_groups][n_best]: the beam 0 .. beams-1 continued, the word, its v, and (NULL: not wanted) out_done =
  * done of the beam, or word == eos (eos < 0: never).  Where there are fewer continuations than n_best, the rest are
- * beam -1, word -1, v = -inf, done 1.  With n_best == beams, out_scores may be scores and out_done may be done (a search that
- * keeps its state in place); no other overlaps.  ws >= fg_beam_select_workspace_bytes, whose size is enough for fewer
- * sequences, beams and n_best of the same cfg too; one ws serves one call at a time. */
+ * beam -1, word -1, v = -inf, done 1.  With n_best == beams, out_scores may be scores and out_done may be done (a
+ * search that keeps its state in place); no other overlaps.  ws >= fg_beam_select_workspace_bytes, whose size is
+ * enough for fewer sequences, beams and n_best of the same cfg too; one ws serves one call at a time. */
 #define FG_MAX_BEST 32
 int fg_beam_select(const fg_model_cfg* cfg, int32_t n_groups, int32_t beams, int32_t n_best, const float* logits,
                    int64_t row_stride, const float* scores, const int32_t* done, int32_t eos, int32_t* out_beams,
@@ -441,21 +447,21 @@ int fg_beam_select(const fg_model_cfg* cfg, int32_t n_groups, int32_t beams, int
 size_t fg_beam_select_workspace_bytes(const fg_model_cfg* cfg, int32_t n_groups, int32_t beams, int32_t n_best);
 
 /* fg_beam_reorder_paged: the caches of all l layers (host array of l pools of one format and page count) behind the
- * beams that were chosen: row i takes over the state of row parents[i] of its group (0 .. beams-1; anything else: its
- * own), i.e. table_out[i] = table_in[parent], pos_out[i] = pos_in[parent] (rows cached), entries past the pages held are -1.
- * Full pages are shared, not copied.  The page where row i's next position goes (slot pos/64) becomes row i's alone:
- * if it is partly filled, the first row of the group that has it there keeps it, unless a row of the group (of greater
- * length) holds it as a full page; the others take a free page and a copy of its filled rows (up to the next multiple
- * of 16) in every layer; if it is not begun, every row takes a free page.
- * Group g owns pages g*pages_per_group .. (g+1)*pages_per_group - 1 of the pools (all below n_pages); free are those
- * that no row of the group holds any more, and the lowest is taken first (so nobody else may hold pages of that range).  Pages outside the group's range (a prompt
- * shared between groups) are only read: a row whose partly filled page lies there takes a copy.  A row that finds no
- * free page, or whose next position is beyond the table, gets no entry there (-1: appending skips it) and counts in
- * missing[g] (int32 per group, or NULL).  pages_per_group = pages of the prompt + beams * (own pages per beam + 1)
- * always suffices.
+ * beams that were chosen: row i takes over the state of row parents[i] of its group (0 .. beams-1; anything else:
+ * its own), i.e. table_out[i] = table_in[parent], pos_out[i] = pos_in[parent] (rows cached), entries past the pages
+ * held are -1. Full pages are shared, not copied.  The page where row i's next position goes (slot pos/64) becomes
+ * row i's alone: if it is partly filled, the first row of the group that has it there keeps it, unless a row of the
+ * group (of greater length) holds it as a full page; the others take a free page and a copy of its filled rows (up
+ * to the next multiple of 16) in every layer; if it is not begun, every row takes a free page. Group g owns pages
+ * g*pages_per_group .. (g+1)*pages_per_group - 1 of the pools (all below n_pages); free are those that no row of
+ * the group holds any more, and the lowest is taken first (so nobody else may hold pages of that range).  Pages
+ * outside the group's range (a prompt shared between groups) are only read: a row whose partly filled page lies
+ * there takes a copy.  A row that finds no free page, or whose next position is beyond the table, gets no entry
+ * there (-1: appending skips it) and counts in missing[g] (int32 per group, or NULL).  pages_per_group = pages of
+ * the prompt + beams * (own pages per beam + 1) always suffices.
  * table_in, pos_in, parents, table_out [rows][table_stride], pos_out: device int32, rows = n_groups * beams; table_out
- * may be table_in and pos_out pos_in, other overlaps are not allowed.  ws >= fg_beam_reorder_workspace_bytes; one ws serves one call at a
- * time. */
+ * may be table_in and pos_out pos_in, other overlaps are not allowed.  ws >= fg_beam_reorder_workspace_bytes; one ws
+ * serves one call at a time. */
 int fg_beam_reorder_paged(const fg_model_cfg* cfg, int32_t l, const fg_kv_pages* pages, int32_t n_groups, int32_t beams,
                           int32_t pages_per_group, const int32_t* parents, const int32_t* table_in,
                           const int32_t* pos_in, int32_t table_stride, int32_t* table_out, int32_t* pos_out,

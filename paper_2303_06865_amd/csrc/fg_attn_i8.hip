@@ -1,30 +1,34 @@
-// Decode attention over 8-bit pages (FG_I8P64): softmax(q K^T / sqrt(dh)) V for one token per row, several rows and query
-// heads on the same keys and values at once.
+// Decode attention over 8-bit pages (FG_I8P64): softmax(q K^T / sqrt(dh)) V for one token per row, several rows and
+// query heads on the same keys and values at once.
 //
-// Both products run on the integer matrix cores, on the stored codes as they are: no code is ever unpacked.  What stands on
-// the other side is a number in four digits:
+// Both products run on the integer matrix cores, on the stored codes as they are: no code is ever unpacked.  What stands
+// on the other side is a number in four digits:
 //   q_d = 2^(E - 30) (sum_t 2^(8t) a_td + r_d / 1024),   -128 <= a_td <= 127,   2^E > max |q|,   |r_d| < 1024
 //   p_j =     1 / Cp * sum_t 2^(7t) b_tj,    0 <= b_tj <= 127,   Cp = 2^28 - 64     (p = 2^(s - max over the page) <= 1)
-// so that q.k = 2^(E - 30) S_k sum_t 2^(8t) (a_t . c) with exact 32-bit integer sums, put together in binary32.  Queries are exact
-// like that: up to a magnitude of 64, 2^(E - 30) is no larger than FP16's smallest step; beyond it the rests r, whole numbers of two
-// more digits, are multiplied where one is not zero.  Weights are off by 2^-28 of the page's largest.  The four
-// digits are four columns of v_mfma_i32_16x16x64_i8; its sixteen columns are four queries: the beams of a sequence that share
-// the page, or the query heads of a cache head, or (one query) idle, at no cost, because the loads are what bounds this.
+// so that q.k = 2^(E - 30) S_k sum_t 2^(8t) (a_t . c) with exact 32-bit integer sums, put together in binary32.
+// Queries are exact like that: up to a magnitude of 64, 2^(E - 30) is no larger than FP16's smallest step; beyond it
+// the rests r, whole numbers of two more digits, are multiplied where one is not zero.  Weights are cut off at 2^-28 of
+// the page's largest: 64 of them are off by 2^-22 of it together.  The four digits are four columns of
+// v_mfma_i32_16x16x64_i8; its sixteen columns are four queries: the beams of a sequence that share the page, or the
+// query heads of a cache head, or (one query) idle, at no cost, because the loads are what bounds this.
 //
 //   S^T[key][column] = K . A^T    rows = keys; row m of block i is key 16 (m / 4) + 4 i + m % 4 of the page, so that lane
 //                                 group g (lane / 16) ends up with keys 16 g .. 16 g + 15, four per block
-//   O^T[d][column] += V^T . B^T   the lane group's 16 weights, packed to bytes, are the operand already; the pages hold the
-//                                 value codes of 16 positions next to each other, which is the other operand
+//   O^T[d][column] += V^T . B^T   the lane group's 16 weights, packed to bytes, are the operand already; the pages hold
+//                                 the value codes of 16 positions next to each other, which is the other operand
 //
-// A unit is (group of rows, cache head, four queries); the units of a cache head are neighbours, so that their waves find its
-// pages in the L1.  WPU waves share a unit's pages round-robin, and SPLITS workgroups where the units are too few for the chip.
-// Each keeps a running (maximum, sum, output) per column; they are merged through LDS, and through memory by a second launch
-// where there are splits.  A wave has the values of a page and the keys of its next one on their way while it computes.
+// A unit is (group of rows, cache head, four queries); the units of a cache head are neighbours, so that their waves
+// find its pages in the L1 where they share a workgroup (one or two waves a unit).  With four waves a unit is a
+// workgroup, and the units of a cache head fetch its pages one by one (4 x 8 beams: 51 MB for 34).  WPU waves share a
+// unit's pages round-robin, and SPLITS workgroups where the units are too few for the chip.  Each keeps a running
+// (maximum, sum, output) per column; they are merged through LDS, and through memory by a second launch where there are
+// splits.  A wave has the values of a page and the keys of its next one on their way while it computes.
 //
-// Bound by the loads where sequences are long: 64 sequences of 1 to 2047 rows, 32 heads of 128, 538 MB: 105 us, 5 TB/s; 16 x 4
-// beams of 512 shared and 30 own rows, 96 heads, 252 MB: 51 us; one sequence of 32768 rows, 32 heads on 8, 67 MB: 15 us and 4 for
-// the merge.  A page costs a wave some 1700 cycles (64 conversions and additions for the scores, 16 exponentials, 64 for the
-// digits, 64 for the output, 16 matrix instructions of 16), a third of what the loads take with all waves of a CU at it.
+// Bound by the loads where sequences are long: 64 sequences of 1 to 2047 rows, 32 heads of 128, 538 MB: 108 us, 5 TB/s;
+// 16 x 4 beams of 512 shared and 30 own rows, 96 heads, 302 MB of pages: 51 us, 6.2 TB/s of what is fetched; one
+// sequence of 32768 rows, 32 heads on 8, 67 MB: 15 us and 4 for the merge.  A page costs a wave some 1700 cycles (64
+// conversions and additions for the scores, 16 exponentials, 64 for the digits, 64 for the output, 16 matrix
+// instructions of 16), a third of what the loads take with all waves of a CU at it.
 #include "fg_attn_common.h"
 
 namespace fg {
@@ -71,16 +75,16 @@ __device__ __forceinline__ int rows_in(const AttnI8Args& a, int cached) {
   return (int)(n < 0 ? 0 : (n > most ? most : n));
 }
 __device__ __forceinline__ int rows_of(const AttnI8Args& a, int row) { return rows_in(a, a.seq_rows[row]); }
-// The same bits in the four lanes: each takes its own digit of what comes of it.  (A product that the compiler fused into the
-// first addition would be rounded in one lane and not in the other.)
+// The same bits in the four lanes: each takes its own digit of what comes of it.  (A product that the compiler fused
+// into the first addition would be rounded in one lane and not in the other.)
 __device__ __forceinline__ float quad_sum(float v) {
   __asm__("" : "+v"(v));
   v += dpp_f32<kDppXor1>(v);
   return v + dpp_f32<kDppXor2>(v);
 }
 
-// The lane's digit of four whole numbers below 2^31 - 2^23, one a byte: with 128 (of each digit) added, digits are from 0.
-// which: 0x0c0c0400 + 0x0101 * digit.
+// The lane's digit of four whole numbers below 2^31 - 2^23, one a byte: with 128 (of each digit) added, digits are from
+// 0. which: 0x0c0c0400 + 0x0101 * digit.
 __device__ __forceinline__ int digits4(const float (&n)[4], uint32_t which) {
   uint32_t u[4];
 #pragma unroll
@@ -123,8 +127,8 @@ __global__ __launch_bounds__(256, 3) void attn_decode_i8_kernel(AttnI8Args a) {
   {
     const half_t* src = a.q + (int64_t)row * a.q_stride + (int64_t)head * DH + 16 * g;
     h8_t x[KS][2];
-    // Magnitudes are ordered as their bits.  An infinity or a NaN in the query makes top infinite, so every score a NaN, so the
-    // output too.
+    // Magnitudes are ordered as their bits.  An infinity or a NaN in the query makes top infinite, so every score a
+    // NaN, so the output too.
     us8_t bits = (us8_t)(uint16_t)0;
 #pragma unroll
     for (int k = 0; k < KS; ++k)
@@ -284,7 +288,8 @@ __global__ __launch_bounds__(256, 3) void attn_decode_i8_kernel(AttnI8Args a) {
       __builtin_amdgcn_sched_barrier(0);
       if (v + 1 < count) load_k(page_n);
       __builtin_amdgcn_sched_barrier(0);
-      // a scale of infinity: NaN, whatever the signs and the weights (digit sums of one sign would give -inf, a weight of 0)
+      // a scale of infinity: NaN, whatever the signs and the weights (digit sums of one sign would give -inf, a weight
+      // of 0)
       const float f = ks < INFINITY ? qmul * ks : NAN;
       float s[4][4];
 #pragma unroll
@@ -441,21 +446,24 @@ struct Plan {
 };
 size_t part_bytes(int64_t rows_heads, int splits, int dh) { return splits > 1 ? align_up((size_t)rows_heads * splits * (dh + 2) * 4, 256) : 0; }
 
-// Waves per unit, and workgroups that share a sequence.  Only the device knows the lengths; what the table could hold stands for
-// them.  Measured, us with 1 / 2 / 4 waves a unit, pages of 64 rows at head size 128 (ordinary loads):
+// Waves per unit, and workgroups that share a sequence.  Only the device knows the lengths; what the table could hold
+// stands for them, in all three rules: a table with room for much more than its sequences hold is planned as a full one.
+// Measured, us with 1 / 2 / 4 waves a unit, pages of 64 rows at head size 128 (ordinary loads):
 //   6144 units, 2 pages 39 / 43 / 54         2048 units, 2 pages 14.4 / 17.6 / 19.5, 7 pages 42.7 / 44.0 / 44.8,
-//   2048 units of 1 to 32 pages (table of 32) 115 / 107 / 104       1536 units of four beams, 8 shared pages 60.9 / 58.3 / 59.6
-//   (57 / 51 / 54 loaded as below)
+//   2048 units of 1 to 32 pages (table of 32) 115 / 107 / 104
+//   1536 units of four beams, 8 shared pages 60.9 / 58.3 / 59.6 (57 / 51 / 54 loaded as below)
 //   768 units of four beams, head size 64, 9 pages 19.2 / 18.4 / 18.0    128 units, 32 pages 39.5 / 23.3 / 15.0
 //   1024 units, four to a cache head (their waves meet in the L1 if they share a workgroup) 46.8 / 50.8 / 81.2
+// (units of one cache head below 1024 have not been compared: there four waves a unit stand for what more waves give)
 // and where units are few, with 1 / 2 / 4 / 8 / 16 / 32 splits of four waves:
-//   128 units, 32 pages 15.0 / 17.0 / 16.7 / 19.2    32 units, 24 pages 17.1 / 16.4 / 15.4 / 14.6, 125 pages 39.6 / 25.4 / 17.7 / 16.8 /
-//   16.5 / 19.0    8 units, 512 pages 144 / 77 / 43 / 26 / 17.7 / 17.4
-// Pages that one wave alone reads are loaded as data that is not needed again, where the call reads more than the last-level cache
-// keeps until the next step; us, with the ordinary loads first: 16 x 4 beams, 96 heads, 252 MB 57.9 / 51.0; 64 sequences of 542
-// rows, 96 heads, 870 MB 152 / 138 (6.3 TB/s).  Below that a program's next step may find the pages there: 4 sequences of 2000 rows,
-// 32 heads, 66 MB, repeated 15.0 / 20.0.  The price: 64 sequences that share 512 rows by fours without saying so 87 / 113; the call
-// with beams is for those.  And where several tiles of queries read a cache head's pages the L1 has to keep them:
+//   128 units, 32 pages 15.0 / 17.0 / 16.7 / 19.2    32 units, 24 pages 17.1 / 16.4 / 15.4 / 14.6
+//   32 units, 125 pages 39.6 / 25.4 / 17.7 / 16.8 / 16.5 / 19.0    8 units, 512 pages 144 / 77 / 43 / 26 / 17.7 / 17.4
+// Pages that one wave alone reads are loaded as data that is not needed again, where the call could read more than the
+// last-level cache keeps until the next step; us, with the ordinary loads first: 16 x 4 beams, 96 heads, 252 MB 57.9 /
+// 51.0; 64 sequences of 542 rows, 96 heads, 870 MB 152 / 138 (6.3 TB/s).  Below that a program's next step may find the
+// pages there: 4 sequences of 2000 rows, 32 heads, 66 MB, 15.0 / 20.0 (one call repeated; in a model the other layers'
+// pages pass between two reads).  The price: 64 sequences that share 512 rows by fours without saying so 87 / 113; the
+// call with beams is for those.  And where several tiles of queries read a cache head's pages the L1 has to keep them:
 // 32 x 4 beams, 32 heads on 8 46 / 60.
 Plan plan_i8(int32_t nh, int32_t nkv, int32_t beams, int32_t b, int32_t dh, int32_t table_stride) {
   Plan p;

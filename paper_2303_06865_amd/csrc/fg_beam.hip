@@ -10,18 +10,22 @@ namespace fg {
 namespace {
 
 // ---------------------------------------------------------------- selection
-// Two launches.  The first reads every logit once: a workgroup takes one piece of one row into registers and leaves the piece's
-// maximum, its sum of exponentials and its n_best words.  The second takes a sequence: what all pieces of all its beams left.
+// Two launches.  The first reads every logit once: a workgroup takes one piece of one row into registers and leaves the
+// piece's maximum, its sum of exponentials and its n_best words.  The second takes a sequence: what all pieces of all
+// its beams left.
 //
-// The n best of a workgroup's values without sorting them: of the largest values of the 64 groups of four threads, the n-th
-// largest is a bound that at least n values reach, and (values falling as they may) few more.  Those are collected in LDS and
-// each counts how many are better: its place.  Should more than kList reach the bound (equal values, mostly), the best are
+// The n best of a workgroup's values without sorting them: of the largest values of the 64 groups of four threads, the
+// n-th largest is a bound that at least n values reach, and (values falling as they may) few more.  Those are collected
+// in LDS and each counts how many are better: its place.  Should more than kList reach the bound (equal values; in the
+// second launch also n = 32 best of some hundred pieces, whose first places all lie with the same threads), the best are
 // taken one after the other instead.  Values carry their place in the key, so no two are equal.
 //
-// The sum of exponentials decides between words of different beams and so is kept better than one binary32 exponential is:
-// exp(y) = 2^h (1 + (y - h ln 2)), y = x - max, h about y log2 e and ln 2 to twice the precision; added up in binary32 over a
-// thread's 8 or 32 values and in binary64 from there on.  What is left are the roundings of y (none for words within a factor of two of the
-// largest) and of the exponential instruction itself, some 2^-24 of each word's share and of either sign.
+// The sum of exponentials decides between words of different beams and so is kept better than one binary32 exponential
+// is: exp(y) = 2^h (1 + (y - h ln 2)), y = x - max, h about y log2 e and ln 2 to twice the precision; added up in
+// binary32 over a thread's 8 or 32 values and in binary64 from there on.  What is left: the roundings of these sums
+// (two a word, 2^-18 in all), of y (none for words within a factor of two of the largest; the mean of |y| is below
+// log(vocab), so 2^-19.7) and of the exponential instruction itself, together below 2^-17 at worst and 2^-21 in what
+// was measured.
 constexpr int kList = 512;
 
 // A forbidden word is -inf (also NaN); +inf counts as the largest finite number.
@@ -40,8 +44,8 @@ __device__ __forceinline__ uint64_t ordered(double x) {
   return u >> 63 ? ~u : u | (1ull << 63);
 }
 
-// Keys: of a piece's words (logit, lower word first); of a sequence's continuations (value, logit, lower beam, lower word).
-// All zero: none.
+// Keys: of a piece's words (logit, lower word first); of a sequence's continuations (value, logit, lower beam, lower
+// word).  All zero: none.
 struct Key1 {
   uint64_t k;
   __device__ __forceinline__ bool operator<(const Key1& o) const { return k < o.k; }
@@ -105,9 +109,9 @@ __device__ __forceinline__ double row16_max_f64(double v) {
 template <class K>
 __device__ __forceinline__ K larger(K a, K b) { return a < b ? b : a; }
 
-// The n (<= 32) largest keys of a workgroup of 256 threads.  mine: the largest of the thread's, or a lower bound of it that one
-// of its keys reaches.  each(bound, f) calls f for every key of the thread that reaches the bound (and may for others, none()
-// included).  emit(place, key) is called once for every place below the number found, which is returned.
+// The n (<= 32) largest keys of a workgroup of 256 threads.  mine: the largest of the thread's, or a lower bound of it
+// that one of its keys reaches.  each(bound, f) calls f for every key of the thread that reaches the bound (and may for
+// others, none() included).  emit(place, key) is called once for every place below the number found, which is returned.
 template <class K, class Each, class Emit>
 __device__ __forceinline__ int block_best(int n, K mine, K* list /* [kList] */, K* tops /* [64] */, K* bound_at, int* count, Each each,
                                           Emit emit) {
@@ -208,8 +212,8 @@ __global__ __launch_bounds__(256) void beam_rows_kernel(SelectArgs a) {
       x[j] = w < n ? src[w] : -INFINITY;
     }
   }
-  // Is there a NaN or +inf?  As whole numbers, +inf and the NaNs above it are the largest with a sign, and the NaNs with the
-  // sign set are above -inf without.
+  // Is there a NaN or +inf?  As whole numbers, +inf and the NaNs above it are the largest with a sign, and the NaNs
+  // with the sign set are above -inf without.
   int most = 0;
   uint32_t most_u = 0;
 #pragma unroll
@@ -265,8 +269,9 @@ __global__ __launch_bounds__(256) void beam_rows_kernel(SelectArgs a) {
   }
 }
 
-// One workgroup per sequence: 7.6 us for 64 sequences of 8 beams x 7 pieces x 16 words, 5.5 for one of 4 x 25 x 4, most of it the
-// latency of loads, logarithms and three barriers behind each other.  HELD: the keys of its continuations fit into LDS (kHeld) and are made once.
+// One workgroup per sequence: 7.6 us for 64 sequences of 8 beams x 7 pieces x 16 words, 5.5 for one of 4 x 25 x 4, most
+// of it the latency of loads, logarithms and three barriers behind each other.  HELD: the keys of its continuations fit
+// into LDS (kHeld) and are made once.
 constexpr int kHeld = 2048;
 template <bool HELD>
 __global__ __launch_bounds__(256) void beam_merge_kernel(SelectArgs a) {
@@ -368,8 +373,9 @@ struct ReorderArgs {
 };
 
 // One workgroup per group.  A thread takes a column of the group's table: it reads the entries of all beams before it
-// writes any, so the table may be rewritten in place.  Pages held are marked in a bitmap in LDS: the full ones first, so that a
-// begun page that somebody holds as a full one is known, then the begun ones.  24 groups of 4: 5.3 us, latency.
+// writes any, so the table may be rewritten in place.  Pages held are marked in a bitmap in LDS: the full ones first,
+// so that a begun page that somebody holds as a full one is known, then the begun ones.  24 groups of 4: 5.3 us,
+// latency.
 __global__ __launch_bounds__(256) void beam_table_kernel(ReorderArgs a) {
   extern __shared__ uint32_t held[];   // one bit per page of the group
   __shared__ int parent[FG_MAX_BEAMS], raw[FG_MAX_BEAMS], last[FG_MAX_BEAMS];
@@ -452,9 +458,10 @@ struct CopyArgs {
   int32_t unit[2];                   // bytes of 16 rows of one head: codes, pairs (0: none; -1: one scale per head)
 };
 
-// How many rows take a copy only the device knows.  A fixed number of workgroups collects those rows (1024 at a time) in LDS and
-// shares out what there is to do: one (copy, layer, tensor, head) after the other, up to 8 KiB each.  30 copies of 48 rows in eight
-// layers of 32 heads of 128, 191 MB: 37 us, 5.2 TB/s (a workgroup per row, layer and tensor: 63).
+// How many rows take a copy only the device knows.  A fixed number of workgroups collects those rows (1024 at a time)
+// in LDS and shares out what there is to do: one (copy, layer, tensor, head) after the other, up to 8 KiB each.  30
+// copies of 48 rows in eight layers of 32 heads of 128, 191 MB: 37 us, 5.2 TB/s (a workgroup per row, layer and tensor:
+// 63).
 __global__ __launch_bounds__(256) void beam_copy_kernel(CopyArgs a) {
   __shared__ int4 list[1024];
   __shared__ int waves[4];
@@ -505,8 +512,8 @@ __global__ __launch_bounds__(256) void beam_copy_kernel(CopyArgs a) {
   }
 }
 
-// Words of a row that a workgroup takes: 8192 where such pieces fill the chip, else 2048 (512 rows of 50272 words, 102 MB: 21.0 us
-// with 8192, 23.7 with 4096; four rows with 2048: 4.3).
+// Words of a row that a workgroup takes: 8192 where such pieces fill the chip, else 2048 (512 rows of 50272 words, 102
+// MB: 21.0 us with 8192, 23.7 with 4096; four rows with 2048: 4.3).
 struct SelectPlan {
   int vpt, pieces, piece;
 };

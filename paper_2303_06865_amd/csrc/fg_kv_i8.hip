@@ -2,9 +2,10 @@
 //
 // A page holds 64 positions; per page, head and tensor one binary32 scale S, codes c with value S c.  The scale follows
 // the largest magnitude stored so far, so a row that exceeds it makes the page's other codes be rounded again to the
-// wider step: rint(c * (S / S')).  That happens about ln(64) times in a page's life when rows come one at a time, and not at
-// all when a page is filled by one call.  Every step of the arithmetic is one rounded binary32 operation (this file is
-// compiled without contraction and with IEEE division), so codes and scales are a function of the call sequence alone.
+// wider step: rint(c * (S / S')).  That happens about ln(64) times in a page's life when rows come one at a time, and
+// not at all when a page is filled by one call.  Every step of the arithmetic is one rounded binary32 operation (this
+// file is compiled without contraction and with IEEE division), so codes and scales are a function of the call sequence
+// alone.
 #include <type_traits>
 
 #include "fg_common.h"
@@ -52,7 +53,8 @@ __device__ __forceinline__ Step step_of(float top, float old, bool begun) {
   s.inv = s.now > 0.f ? 1.0f / s.now : 0.f;
   return s;
 }
-// rint in one addition: 1.5 * 2^23 + y has the whole number in its low bits, two's complement (the code is the lowest byte)
+// rint in one addition: 1.5 * 2^23 + y has the whole number in its low bits, two's complement (the code is the lowest
+// byte)
 __device__ __forceinline__ uint32_t whole(float y) { return __builtin_bit_cast(uint32_t, y + 12582912.0f); }
 // (the FMA with nothing is the product, rounded once, taken from FP16 as it is)
 __device__ __forceinline__ uint32_t code_of(half_t v, const Step& s) { return whole(__builtin_fmaf((float)v, s.inv, 0.f)); }
@@ -84,17 +86,18 @@ __device__ __forceinline__ u2_t codes_again(u2_t c, const Step& s) {
   return c;
 }
 
-// The units of 16 positions of a page's value codes in LDS, [group of 16][dh] in an order in which the lanes that hold eight
-// neighbouring dimensions each, as well as lanes that take units in order, meet few others on a bank.
+// The units of 16 positions of a page's value codes in LDS, [group of 16][dh] in an order in which the lanes that hold
+// eight neighbouring dimensions each, as well as lanes that take units in order, meet few others on a bank.
 template <int DH>
 __device__ __forceinline__ int unit_at(int group, int d) {
   return (group * DH + (d & ~7) + (((d & 7) + (d >> 3)) & 7)) * 16;
 }
 
-// One workgroup per (sequence of the call, page it touches, head, K or V), a wave per group of 16 positions; lane = 8 head dimensions
-// (lane % LR) of RPL positions.  The new rows stay in registers until the page's largest magnitude is known.  Value codes pass
-// through LDS and leave in their units, in order.  Storing 16 x 500 rows of 32 heads: with units straight from the lanes, 16
-// bytes in every 128, 70 us; in order, a wave per page 54; this 52, 3.8 TB/s of rows read and codes written.
+// One workgroup per (sequence of the call, page it touches, head, K or V), a wave per group of 16 positions; lane = 8
+// head dimensions (lane % LR) of RPL positions.  The new rows stay in registers until the page's largest magnitude is
+// known.  Value codes pass through LDS and leave in their units, in order.  Storing 16 x 500 rows of 32 heads: with
+// units straight from the lanes, 16 bytes in every 128, 70 us; in order, a wave per page 54; this 52, 3.8 TB/s of rows
+// read and codes written.
 template <int DH, bool VALUES>
 __device__ __forceinline__ void store_rows(const half_t* src, int64_t ld, int8_t* codes, float* scale, int lo, int hi, int lane,
                                            int q, uint8_t* sm, float* sm_top) {
@@ -195,8 +198,8 @@ __global__ __launch_bounds__(256) void kv_append_i8_kernel(AppendI8Args a) {
   const int64_t ph = (int64_t)page * a.nh + head;
   int8_t* codes = a.codes[which] + ph * (FG_PAGE_ROWS * DH);
   float* scale = a.scales[which] + ph;
-  // A sequence that is named more than once: the first of its rows that touches the page stores them all, in order.  (Everything
-  // that decides is the same in all four waves.)
+  // A sequence that is named more than once: the first of its rows that touches the page stores them all, in order.
+  // (Everything that decides is the same in all four waves.)
   const int from = a.at.seq_ids ? 0 : i, to = a.at.seq_ids ? a.b : i + 1;
   for (int base = from; base < to; base += 64) {
     const int jl = base + lane;
@@ -220,9 +223,9 @@ __global__ __launch_bounds__(256) void kv_append_i8_kernel(AppendI8Args a) {
   }
 }
 
-// One new row per sequence (the decode step): DH / 8 lanes a head, eight or four heads a wave, K or V.  What is written are eight
-// bytes a lane, for V in eight units; only a page whose scale grows is read.  64 sequences x 32 heads of 128: 6 us, the latency of
-// position, page and row behind each other (a wave per head and page: 17).
+// One new row per sequence (the decode step): DH / 8 lanes a head, eight or four heads a wave, K or V.  What is written
+// are eight bytes a lane, for V in eight units; only a page whose scale grows is read.  64 sequences x 32 heads of 128:
+// 6 us, the latency of position, page and row behind each other (a wave per head and page: 17).
 template <int DH>
 __global__ __launch_bounds__(256) void kv_append_i8_row_kernel(AppendI8Args a) {
   constexpr int LR = DH / 8, HPW = 64 / LR;
@@ -296,10 +299,11 @@ struct GatherArgs {
   PageRows at;
 };
 
-// One workgroup per (sequence of the call, page, head, K or V), a wave per group of 16 positions; lane = 8 head dimensions
-// (lane % LR) of RPL positions.  Waves whose group nobody asked for have nothing to do.  The 8-bit value codes come in their
-// units, in order, and pass through LDS.  8 x 1500 rows of 32 heads of 128, 295 MB: 59 us, 5.0 TB/s (a wave per page, all 64
-// positions' loads first, 133 registers: 62); 16 x 400 rows of 56 heads from 4.5-bit pages, 235 MB: 51 us (58).
+// One workgroup per (sequence of the call, page, head, K or V), a wave per group of 16 positions; lane = 8 head
+// dimensions (lane % LR) of RPL positions.  Waves whose group nobody asked for have nothing to do.  The 8-bit value
+// codes come in their units, in order, and pass through LDS.  8 x 1500 rows of 32 heads of 128, 295 MB: 59 us, 5.0 TB/s
+// (a wave per page, all 64 positions' loads first, 133 registers: 62); 16 x 400 rows of 56 heads from 4.5-bit pages,
+// 235 MB: 51 us (58).
 template <int DH, int FMT>
 __global__ __launch_bounds__(256) void kv_gather_kernel(GatherArgs a) {
   constexpr int LR = DH / 8, RPL = LR / 4, UPL = DH / 64;   // positions, units per lane
