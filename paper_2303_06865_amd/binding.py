@@ -536,6 +536,7 @@ def fg_decode_layer(cfg: Cfg, w: LayerWeights, x: torch.Tensor, t: int, kv: KVCa
 def fg_kv_append_paged(cfg: Cfg, k: torch.Tensor, v: torch.Tensor, row_stride: int, b: int, s: int, pages: KVPages,
                        seqs: Ragged) -> None:
     pages.check(cfg.nh, cfg.dh)
+    seqs.check(b)
     _check(lib().fg_kv_append_paged(C.byref(cfg.c), _p(k), _p(v), row_stride, b, s, C.byref(pages.c), C.byref(seqs.c),
                                     _stream()), "fg_kv_append_paged")
 
@@ -543,6 +544,7 @@ def fg_kv_append_paged(cfg: Cfg, k: torch.Tensor, v: torch.Tensor, row_stride: i
 def fg_decode_attention_paged(cfg: Cfg, q: torch.Tensor, q_row_stride: int, b: int, pages: KVPages, seqs: Ragged,
                               rows_bias: int = 0) -> torch.Tensor:
     pages.check(cfg.nh, cfg.dh)
+    seqs.check(b)
     out = torch.empty((b, cfg.h1), dtype=torch.float16, device=q.device)
     _check(lib().fg_decode_attention_paged(C.byref(cfg.c), _p(q), q_row_stride, b, C.byref(pages.c), C.byref(seqs.c),
                                            rows_bias, _p(out), _stream()), "fg_decode_attention_paged")
@@ -700,6 +702,7 @@ def fg_decode_layer_paged(cfg: Cfg, w: LayerWeights, x: torch.Tensor, pages: KVP
     pages.check(cfg.nh, cfg.dh)
     x = _f16(x)
     b = x.shape[0]
+    seqs.check(b)
     if out is None:
         out = torch.empty_like(x)
     if ws is None:

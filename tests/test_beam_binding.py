@@ -91,6 +91,15 @@ def test_attention_refuses_less_than_its_rows():
         att(CFG, 4, 2, q, 768, 4, pool, _seqs(4), out=torch.zeros((4, 256)))
 
 
+def test_rows_that_nobody_names_are_refused():
+    pool, q = _pool(), torch.zeros((4, 768), **HALF)
+    for seqs in (_seqs(3), _seqs(4, ids=3)):
+        for call in (lambda: B.fg_kv_append_paged(CFG, q[:, 256:], q[:, 512:], 768, 4, 1, pool, seqs),
+                     lambda: B.fg_decode_attention_paged(CFG, q, 768, 4, pool, seqs)):
+            with pytest.raises(AssertionError, match="name all 4 rows"):
+                call()
+
+
 def test_gather_refuses_tensors_that_do_not_hold_its_rows():
     pool, ga = _pool(), B.fg_kv_gather_paged
     k = torch.zeros((2, 3, 256), **HALF)
